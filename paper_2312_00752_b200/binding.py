@@ -1,6 +1,7 @@
-"""Thin Python binding of the C ABI in include/ssm_scan.h (same names, argument marshalling only).
+"""Thin Python binding of the C ABI in include/ (ssm_scan.h, ssm_conv1d.h, ssm_gated.h, ssm_norm.h; same names, argument
+marshalling only).
 
-Every step of the selective scan runs in the CUDA kernels of libssm_scan.so; torch is used for device memory and
+Every step of the selective scan and its neighbours runs in the CUDA kernels of libssm_scan.so; torch is used for device memory and
 streams.  There is no CPU or eager fallback: if the library is missing or fails to load, importing a symbol raises.
 The calls that launch kernels marshal their arguments in a compiled module (csrc/marshal.cpp); queries, and the call on
 host buffers, go through ctypes.
@@ -30,11 +31,15 @@ EXPORTED_SYMBOLS = (
     "ssm_scan_fwd_static", "ssm_scan_check_status", "ssm_scan_fwd_state", "ssm_step",
     "ssm_scan_fwd_fused_dt", "ssm_scan_bwd_fused_dt", "ssm_scan_host_arena_bytes", "ssm_scan_fwd_bwd_host",
     "ssm_scan_bwd_state", "ssm_scan_bwd_fused_dt_state", "ssm_conv1d_fwd", "ssm_conv1d_bwd_workspace_bytes", "ssm_conv1d_bwd",
+    "ssm_gated_saved_state_bytes", "ssm_gated_fwd", "ssm_gated_bwd_workspace_bytes", "ssm_gated_bwd", "ssm_gated_step",
+    "ssm_norm_fwd", "ssm_norm_bwd_workspace_bytes", "ssm_norm_bwd",
 )
 SSM_STATIC_SCRATCH_BYTES = 4 << 20
 
 
 SSM_CONV_FLAG_SILU, SSM_CONV_FLAG_HAS_BIAS = 1, 2
+SSM_GATED_FLAG_DECAY, SSM_GATED_FLAG_SAVE_STATES = 1, 4
+SSM_NORM_FLAG_RMS, SSM_NORM_FLAG_HAS_BIAS, SSM_NORM_FLAG_HAS_RESIDUAL = 1, 2, 4
 
 
 class ssm_conv_problem_t(ctypes.Structure):
@@ -45,6 +50,18 @@ class ssm_conv_problem_t(ctypes.Structure):
 class ssm_problem_t(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32), ("N", ctypes.c_int32),
                 ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class ssm_gated_problem_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("ld_x", ctypes.c_int64), ("ld_gate", ctypes.c_int64),
+                ("ld_in_gate", ctypes.c_int64), ("ld_dx", ctypes.c_int64), ("ld_dgate", ctypes.c_int64),
+                ("ld_din_gate", ctypes.c_int64)]
+
+
+class ssm_norm_problem_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("D", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("residual_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("eps", ctypes.c_float)]
 
 
 class SsmScanError(RuntimeError):
@@ -98,6 +115,21 @@ def load_library() -> ctypes.CDLL:
     lib.ssm_conv1d_bwd_workspace_bytes.argtypes = [CP]
     lib.ssm_conv1d_bwd.restype = ctypes.c_int
     lib.ssm_conv1d_bwd.argtypes = [CP] + [vp] * 9 + [vp, sz, vp]
+    GP, NP = ctypes.POINTER(ssm_gated_problem_t), ctypes.POINTER(ssm_norm_problem_t)
+    for name, problem in (("ssm_gated_saved_state_bytes", GP), ("ssm_gated_bwd_workspace_bytes", GP),
+                          ("ssm_norm_bwd_workspace_bytes", NP)):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [problem]
+    lib.ssm_gated_fwd.restype = ctypes.c_int
+    lib.ssm_gated_fwd.argtypes = [GP] + [vp] * 9 + [vp]
+    lib.ssm_gated_bwd.restype = ctypes.c_int
+    lib.ssm_gated_bwd.argtypes = [GP] + [vp] * 14 + [vp, sz, vp]
+    lib.ssm_gated_step.restype = ctypes.c_int
+    lib.ssm_gated_step.argtypes = [GP] + [vp] * 7 + [vp]
+    lib.ssm_norm_fwd.restype = ctypes.c_int
+    lib.ssm_norm_fwd.argtypes = [NP] + [vp] * 7 + [vp]
+    lib.ssm_norm_bwd.restype = ctypes.c_int
+    lib.ssm_norm_bwd.argtypes = [NP] + [vp] * 9 + [vp, sz, vp]
     lib.ssm_scan_bwd_fused_dt_state.restype = ctypes.c_int
     lib.ssm_scan_bwd_fused_dt_state.argtypes = [P] + [vp] * 21 + [vp, sz, vp]
     lib.ssm_scan_bwd_state.restype = ctypes.c_int
@@ -373,3 +405,59 @@ def ssm_conv1d_bwd(x, w, bias, dy, *, silu=True, x_prev=None, want_dx_prev=False
     """Gradients of sum(dy * y) of ssm_conv1d_fwd: dict with dx (io dtype), dw (D, W) and dbias (D) float32 (dbias None
     without bias), and dx_prev (batch, W-1, D) if asked for."""
     return (_marshal_module or _native()).conv_bwd(x, w, bias, x_prev, dy, stream, dict(outputs or {}), silu, want_dx_prev)
+
+
+def ssm_gated_fwd(x, gate, in_gate=None, A=None, *, reset=None, h0=None, h_last=None, save_states=False, out=None,
+                  saved_states=None, stream=None):
+    """Gated linear recurrence h_t = a_t h_{t-1} + u_t, out = h, see include/ssm_gated.h.  Without in_gate and A: a = 1 - g,
+    u = g x with g = sigmoid(gate).  With them: a = exp(sigmoid(gate) A), u = sqrt(1 - a^2) sigmoid(in_gate) x.
+
+    x, gate, in_gate: (batch, L, D) io dtype, whose rows may lie further apart than D (column ranges of one projection's
+    result); A: (D,) float32, not above 0; reset: (batch, L) bool or uint8, the state is taken as zero before the steps where it is
+    set; h0 (batch, D) float32 (default zero); a float32 tensor `h_last` (batch, D) that is passed receives the state after the
+    last step.  Returns `out`, or `(out, saved_states)` with save_states=True.  Enqueues on `stream` (default: torch's
+    current stream of x's device) and does not synchronise.
+    """
+    return (_marshal_module or _native()).gated_fwd(x, gate, in_gate, A, reset, h0, out, h_last, saved_states, stream,
+                                                    save_states)
+
+
+def ssm_gated_bwd(x, gate, in_gate, A, dy, saved_states=None, *, reset=None, h0=None, dh_last=None, want_dh0=False,
+                  outputs=None, stream=None):
+    """Gradients of sum(dy * out) (+ sum(dh_last * h_last)) of ssm_gated_fwd with the same x, gate, in_gate, A, reset and h0;
+    saved_states as that call returned them, or None (they are rebuilt).  Returns a dict with dx, dgate and din_gate (io
+    dtype), dA (D,) and dh0 (batch, D) float32; din_gate and dA are None without in_gate and A, dh0 unless asked for.
+    `outputs` may pass preallocated tensors; the rows of dx, dgate and din_gate may lie further apart than D.
+    """
+    return (_marshal_module or _native()).gated_bwd(x, gate, in_gate, A, dy, saved_states, reset, h0, dh_last, stream,
+                                                    dict(outputs or {}), want_dh0)
+
+
+def ssm_gated_step(x, gate, in_gate, A, h, *, reset=None, out=None, stream=None):
+    """One step of ssm_gated_fwd: x, gate, in_gate (batch, D) io dtype (in_gate and A None together), reset (batch,); h
+    (batch, D) float32 is updated in place.  Returns out (batch, D)."""
+    return (_marshal_module or _native()).gated_step(x, gate, in_gate, A, h, reset, out, stream)
+
+
+def ssm_norm_fwd(x, weight, bias=None, residual=None, *, rms=False, eps=1e-5, save_stats=False, out=None, residual_out=None,
+                 stats=None, stream=None):
+    """Norm of the rows of s = x + residual: out = (s - mean) / sqrt(var + eps) * weight + bias, with rms=True without
+    the mean; see include/ssm_norm.h.
+
+    x: (..., D) io dtype; residual: the same shape, io dtype or float32 (s is rounded to its type); weight, bias: (D,)
+    float32.  Returns `out`; with a residual `(out, residual_out)`, the latter holding s; with save_stats=True the statistics
+    (..., 2) that ssm_norm_bwd needs come last in the tuple.  Enqueues on `stream` (default: torch's current stream of x's device)
+    and does not synchronise.
+    """
+    return (_marshal_module or _native()).norm_fwd(x, weight, bias, residual, out, residual_out, stats, stream, rms, eps,
+                                                   save_stats)
+
+
+def ssm_norm_bwd(s, weight, dy, stats, dresidual_out=None, *, rms=False, has_bias=False, outputs=None, stream=None):
+    """Gradients of sum(dy * out) (+ sum(dresidual_out * residual_out)) of ssm_norm_fwd.  s: its residual_out, or x where there
+    was no residual; dy (..., D) io dtype; stats as that call returned them; dresidual_out (..., D) of s's type or None.
+    Returns a dict with dx (io dtype), dresidual (s's type; the same tensor as dx where the types agree), dweight and dbias (D,)
+    float32 (dbias None without has_bias).  `outputs` may pass preallocated tensors.
+    """
+    return (_marshal_module or _native()).norm_bwd(s, weight, dy, stats, dresidual_out, stream, dict(outputs or {}), rms,
+                                                   has_bias)

@@ -1,7 +1,7 @@
 // Argument marshalling of the Python binding: torch tensors to the pointers of the C ABI (include/ssm_scan.h,
-// include/ssm_conv1d.h), output and workspace allocation.  A CPython module, because the same work in Python (about twelve
-// tensors of a call checked attribute by attribute, the ctypes conversions) cost 12 to 40 us a call, more than a decoding
-// step or a short prompt takes on the GPU.  Nothing of the method is here: the library is loaded by path at import and
+// include/ssm_conv1d.h, include/ssm_gated.h, include/ssm_norm.h), output and workspace allocation.  A CPython module,
+// because the same work in Python (about twelve tensors of a call checked attribute by attribute, the ctypes conversions)
+// cost 12 to 40 us a call, more than a decoding step or a short prompt takes on the GPU.  Nothing of the method is here: the library is loaded by path at import and
 // every call ends in one call of the C ABI.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -20,6 +20,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "ssm_conv1d.h"
+#include "ssm_gated.h"
+#include "ssm_norm.h"
 #include "ssm_scan.h"
 
 namespace {
@@ -32,7 +34,9 @@ PyObject* g_out_of_memory = nullptr;   // torch.OutOfMemoryError
   X(ssm_scan_fwd_state) X(ssm_scan_fwd_fused_dt) X(ssm_scan_fwd_static) X(ssm_scan_bwd) X(ssm_scan_bwd_state)     \
   X(ssm_scan_bwd_fused_dt) X(ssm_scan_bwd_fused_dt_state) X(ssm_step) X(ssm_scan_fwd_workspace_bytes)             \
   X(ssm_scan_bwd_workspace_bytes) X(ssm_scan_saved_state_bytes) X(ssm_status_string) X(ssm_conv1d_fwd)            \
-  X(ssm_conv1d_bwd) X(ssm_conv1d_bwd_workspace_bytes)
+  X(ssm_conv1d_bwd) X(ssm_conv1d_bwd_workspace_bytes) X(ssm_gated_saved_state_bytes) X(ssm_gated_fwd)             \
+  X(ssm_gated_bwd_workspace_bytes) X(ssm_gated_bwd) X(ssm_gated_step) X(ssm_norm_fwd)                             \
+  X(ssm_norm_bwd_workspace_bytes) X(ssm_norm_bwd)
 struct Api {
 #define X(name) decltype(&::name) name;
   SSM_ENTRY_POINTS(X)
@@ -496,6 +500,341 @@ PyObject* conv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------- gated linear recurrence, norm
+const at::Tensor& first(PyObject* o, const char* name) {
+  const at::Tensor* t = tensor(o, name);
+  if (t == nullptr || !t->is_cuda()) raise(std::string(name) + " must be a CUDA tensor");
+  return *t;
+}
+
+// a dimension of the C ABI's 32 bits
+int32_t dimension(int64_t n, const char* what) {
+  if (n > INT32_MAX) raise(std::string(what) + " is too large");
+  return (int32_t)n;
+}
+
+// device pointer of a dense tensor on the device of the call (null for None)
+void* dense(const at::Tensor* t, const char* name, at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& x) {
+  void* p = pointer(t, name, shape, dtype);
+  if (t != nullptr && t->device() != x.device()) raise(std::string(name) + " must be on the device of the other tensors");
+  return p;
+}
+void* dense(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& x) {
+  return dense(tensor(o, name), name, shape, dtype, x);
+}
+float* dense_float(PyObject* o, const char* name, at::IntArrayRef shape, const at::Tensor& x) {
+  return static_cast<float*>(dense(o, name, shape, at::kFloat, x));
+}
+
+// device pointer of a tensor whose rows (the last dimension) are dense and lie evenly spaced, and their distance
+void* spaced(const at::Tensor* t, const char* name, at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& x, int64_t* distance) {
+  *distance = 0;
+  if (t == nullptr) return nullptr;
+  if (!t->is_cuda()) raise(std::string(name) + " must be a CUDA tensor");
+  if (t->device() != x.device()) raise(std::string(name) + " must be on the device of the other tensors");
+  if (t->sizes() != shape) raise(std::string(name) + " has shape " + shape_text(t->sizes()) + ", expected " + shape_text(shape));
+  if (t->scalar_type() != dtype)
+    raise(std::string(name) + " has dtype " + dtype_name(t->scalar_type()) + ", expected " + dtype_name(dtype));
+  const int64_t D = shape.back();
+  bool ok = D <= 1 || t->stride(-1) == 1;
+  int64_t rows = 1, ld = D;     // rows within the dimensions so far, from the last but one outwards, and their distance
+  for (int64_t k = (int64_t)shape.size() - 2; k >= 0; --k) {
+    if (shape[k] == 1) continue;
+    if (rows == 1) ld = t->stride(k);
+    else ok = ok && t->stride(k) == rows * ld;
+    rows *= shape[k];
+  }
+  if (!ok || (rows > 1 && ld < D)) raise(std::string(name) + " must have contiguous rows, evenly spaced");
+  *distance = ld;
+  return t->data_ptr();
+}
+void* spaced(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& x, int64_t* distance) {
+  return spaced(tensor(o, name), name, shape, dtype, x, distance);
+}
+
+// one byte per step
+const uint8_t* mask(PyObject* o, const char* name, at::IntArrayRef shape, const at::Tensor& x) {
+  const at::Tensor* t = tensor(o, name);
+  if (t == nullptr) return nullptr;
+  const bool byte = t->scalar_type() == at::kByte;
+  return static_cast<const uint8_t*>(dense(t, name, shape, byte ? at::kByte : at::kBool, x));
+}
+
+ssm_gated_problem_t gated_problem(const at::Tensor& x, int dims, PyObject* in_gate, PyObject* A) {
+  if (x.dim() != dims) raise("x must have " + std::to_string(dims) + " dimensions");
+  if ((in_gate == Py_None) != (A == Py_None)) raise("in_gate and A are given together (the decay form) or not at all");
+  ssm_gated_problem_t p{};
+  p.batch = dimension(x.size(0), "batch");
+  p.L = dims == 3 ? dimension(x.size(1), "L") : 1;
+  p.D = dimension(x.size(-1), "D");
+  p.io_dtype = io_dtype(x);
+  p.flags = A != Py_None ? SSM_GATED_FLAG_DECAY : 0u;
+  return p;
+}
+
+// gated_fwd(x, gate, in_gate, A, reset, h0, out, h_last, saved_states, stream, save_states) -> out or (out, saved_states)
+PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "gated_fwd: 11 arguments");
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& x = first(a[0], "x");
+    const c10::cuda::CUDAGuard on(x.device());
+    const bool save = truth(a[10]);
+    ssm_gated_problem_t p = gated_problem(x, 3, a[2], a[3]);
+    if (save) p.flags |= SSM_GATED_FLAG_SAVE_STATES;
+    const at::ScalarType io = x.scalar_type();
+    const int64_t B = p.batch, L = p.L, D = p.D;
+    void* px = spaced(&x, "x", {B, L, D}, io, x, &p.ld_x);
+    void* pg = spaced(a[1], "gate", {B, L, D}, io, x, &p.ld_gate);
+    void* pi = spaced(a[2], "in_gate", {B, L, D}, io, x, &p.ld_in_gate);
+    const float* pA = dense_float(a[3], "A", {D}, x);
+    const uint8_t* pr = mask(a[4], "reset", {B, L}, x);
+    const float* ph = dense_float(a[5], "h0", {B, D}, x);
+    float* pl = dense_float(a[7], "h_last", {B, D}, x);
+    if (pg == nullptr) raise("gate must be a CUDA tensor");
+    void* stream = stream_of(a[9], x);
+    const at::Tensor* given = tensor(a[6], "out");
+    const at::Tensor out = given != nullptr ? *given : result({B, L, D}, io, x, stream);
+    void* po = dense(&out, "out", {B, L, D}, io, x);
+    at::Tensor saved;
+    if (save) {
+      const int64_t count = (int64_t)(api.ssm_gated_saved_state_bytes(&p) / 4);
+      const at::Tensor* sgiven = tensor(a[8], "saved_states");
+      saved = sgiven != nullptr ? *sgiven : result({count}, at::kFloat, x, stream);
+      dense(&saved, "saved_states", {count}, at::kFloat, x);
+    }
+    float* ps = save ? static_cast<float*>(saved.data_ptr()) : nullptr;
+    call("ssm_gated_fwd", nullptr, [&] { return api.ssm_gated_fwd(&p, px, pg, pi, pA, pr, ph, po, pl, ps, stream); });
+    if (!save) return wrap(out);
+    PyObject* o = wrap(out);
+    PyObject* sv = wrap(saved);
+    PyObject* r = PyTuple_Pack(2, o, sv);
+    Py_DECREF(o);
+    Py_DECREF(sv);
+    return r;
+  });
+}
+
+// a gradient whose rows may be spaced: the tensor of `outputs` under that name, or a new dense one, which is put there
+at::Tensor spaced_output(PyObject* outputs, const char* name, at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& like,
+                         void* stream, int64_t* distance) {
+  PyObject* have = PyDict_GetItemString(outputs, name);
+  if (have != nullptr && have != Py_None) {
+    const at::Tensor t = *tensor(have, name);
+    spaced(&t, name, shape, dtype, like, distance);
+    return t;
+  }
+  *distance = 0;
+  return output(outputs, name, shape, dtype, like, stream);
+}
+at::Tensor dense_output(PyObject* outputs, const char* name, at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& like,
+                        void* stream) {
+  const at::Tensor t = output(outputs, name, shape, dtype, like, stream);
+  dense(&t, name, shape, dtype, like);
+  return t;
+}
+
+// gated_bwd(x, gate, in_gate, A, dy, saved_states, reset, h0, dh_last, stream, outputs, want_dh0): fills and returns `outputs`
+PyObject* gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 12) return PyErr_Format(PyExc_TypeError, "gated_bwd: 12 arguments");
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& x = first(a[0], "x");
+    const c10::cuda::CUDAGuard on(x.device());
+    ssm_gated_problem_t p = gated_problem(x, 3, a[2], a[3]);
+    if (a[5] != Py_None) p.flags |= SSM_GATED_FLAG_SAVE_STATES;
+    const bool dec = p.flags & SSM_GATED_FLAG_DECAY;
+    const at::ScalarType io = x.scalar_type();
+    const int64_t B = p.batch, L = p.L, D = p.D;
+    void* px = spaced(&x, "x", {B, L, D}, io, x, &p.ld_x);
+    void* pg = spaced(a[1], "gate", {B, L, D}, io, x, &p.ld_gate);
+    void* pi = spaced(a[2], "in_gate", {B, L, D}, io, x, &p.ld_in_gate);
+    const float* pA = dense_float(a[3], "A", {D}, x);
+    void* pdy = dense(a[4], "dy", {B, L, D}, io, x);
+    const float* ps = dense_float(a[5], "saved_states", {(int64_t)(api.ssm_gated_saved_state_bytes(&p) / 4)}, x);
+    const uint8_t* pr = mask(a[6], "reset", {B, L}, x);
+    const float* ph = dense_float(a[7], "h0", {B, D}, x);
+    const float* pm = dense_float(a[8], "dh_last", {B, D}, x);
+    if (pg == nullptr) raise("gate must be a CUDA tensor");
+    if (pdy == nullptr) raise("dy must be a CUDA tensor");
+    void* stream = stream_of(a[9], x);
+    PyObject* o = a[10];
+    const at::Tensor dx = spaced_output(o, "dx", {B, L, D}, io, x, stream, &p.ld_dx);
+    const at::Tensor dg = spaced_output(o, "dgate", {B, L, D}, io, x, stream, &p.ld_dgate);
+    at::Tensor di, dA, dh;
+    if (dec) {
+      di = spaced_output(o, "din_gate", {B, L, D}, io, x, stream, &p.ld_din_gate);
+      dA = dense_output(o, "dA", {D}, at::kFloat, x, stream);
+    } else {
+      no_output(o, "din_gate");
+      no_output(o, "dA");
+    }
+    if (truth(a[11])) dh = dense_output(o, "dh0", {B, D}, at::kFloat, x, stream);
+    else no_output(o, "dh0");
+    auto data = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const Workspace own = workspace(api.ssm_gated_bwd_workspace_bytes(&p), x, stream);
+    call("ssm_gated_bwd", own.enqueue, [&] {
+      return api.ssm_gated_bwd(&p, px, pg, pi, pA, pr, ph, pdy, pm, ps, data(dx), data(dg), data(di),
+                               static_cast<float*>(data(dA)), static_cast<float*>(data(dh)), data(own.buffer),
+                               own.buffer.defined() ? (size_t)own.buffer.numel() : 0, stream);
+    });
+    Py_INCREF(o);
+    return o;
+  });
+}
+
+// gated_step(x, gate, in_gate, A, h, reset, out, stream) -> out
+PyObject* gated_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "gated_step: 8 arguments");
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& x = first(a[0], "x");
+    const c10::cuda::CUDAGuard on(x.device());
+    ssm_gated_problem_t p = gated_problem(x, 2, a[2], a[3]);
+    const at::ScalarType io = x.scalar_type();
+    const int64_t B = p.batch, D = p.D;
+    void* px = spaced(&x, "x", {B, D}, io, x, &p.ld_x);
+    void* pg = spaced(a[1], "gate", {B, D}, io, x, &p.ld_gate);
+    void* pi = spaced(a[2], "in_gate", {B, D}, io, x, &p.ld_in_gate);
+    const float* pA = dense_float(a[3], "A", {D}, x);
+    float* ph = dense_float(a[4], "h", {B, D}, x);
+    const uint8_t* pr = mask(a[5], "reset", {B}, x);
+    if (pg == nullptr) raise("gate must be a CUDA tensor");
+    if (ph == nullptr) raise("h must be a CUDA tensor");
+    void* stream = stream_of(a[7], x);
+    const at::Tensor* given = tensor(a[6], "out");
+    const at::Tensor out = given != nullptr ? *given : result({B, D}, io, x, stream);
+    void* po = dense(&out, "out", {B, D}, io, x);
+    call("ssm_gated_step", nullptr, [&] { return api.ssm_gated_step(&p, px, pg, pi, pA, pr, ph, po, stream); });
+    return wrap(out);
+  });
+}
+
+ssm_norm_problem_t norm_problem(const at::Tensor& x, at::ScalarType residual, uint32_t flags, double eps) {
+  if (x.dim() < 1) raise("x must have at least one dimension");
+  ssm_norm_problem_t p{};
+  p.D = dimension(x.size(-1), "D");
+  p.rows = 1;
+  for (int64_t k = 0; k + 1 < x.dim(); ++k) p.rows *= x.size(k);
+  p.io_dtype = io_dtype(x);
+  p.residual_dtype = residual == at::kFloat ? SSM_F32 : SSM_BF16;
+  p.flags = flags;
+  p.eps = (float)eps;
+  return p;
+}
+c10::SmallVector<int64_t, 6> stats_shape(const at::Tensor& x) {
+  c10::SmallVector<int64_t, 6> s(x.sizes().begin(), x.sizes().end());
+  s.back() = 2;
+  return s;
+}
+// the residual stream's element type: that of the activations, or float32
+at::ScalarType residual_type(const at::Tensor& t, const char* name, at::ScalarType io) {
+  const at::ScalarType r = t.scalar_type();
+  if (r != io && r != at::kFloat) raise(std::string(name) + " has dtype " + dtype_name(r) + ", expected " + dtype_name(io) + " or torch.float32");
+  return r;
+}
+
+// norm_fwd(x, weight, bias, residual, out, residual_out, stats, stream, rms, eps, save_stats) -> out, or a tuple of out, residual_out
+// (with a residual) and stats (with save_stats)
+PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "norm_fwd: 11 arguments");
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& x = first(a[0], "x");
+    const c10::cuda::CUDAGuard on(x.device());
+    io_dtype(x);
+    const at::ScalarType io = x.scalar_type();
+    const at::Tensor* res = tensor(a[3], "residual");
+    const at::ScalarType rt = res != nullptr ? residual_type(*res, "residual", io) : io;
+    const double eps = PyFloat_AsDouble(a[9]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Raised{};
+    const ssm_norm_problem_t p = norm_problem(x, rt, (truth(a[8]) ? SSM_NORM_FLAG_RMS : 0u) | (a[2] != Py_None ? SSM_NORM_FLAG_HAS_BIAS : 0u) |
+                                                         (res != nullptr ? SSM_NORM_FLAG_HAS_RESIDUAL : 0u), eps);
+    const int64_t D = p.D;
+    void* px = dense(&x, "x", x.sizes(), io, x);
+    const float* pw = dense_float(a[1], "weight", {D}, x);
+    const float* pb = dense_float(a[2], "bias", {D}, x);
+    void* pr = dense(res, "residual", x.sizes(), rt, x);
+    if (pw == nullptr) raise("weight must be a CUDA tensor");
+    if (res == nullptr && a[5] != Py_None) raise("residual_out needs a residual");
+    const bool save = truth(a[10]);
+    void* stream = stream_of(a[7], x);
+    const at::Tensor* given = tensor(a[4], "out");
+    const at::Tensor out = given != nullptr ? *given : result(x.sizes(), io, x, stream);
+    void* po = dense(&out, "out", x.sizes(), io, x);
+    at::Tensor sum, stats;
+    if (res != nullptr) {
+      const at::Tensor* t = tensor(a[5], "residual_out");
+      sum = t != nullptr ? *t : result(x.sizes(), rt, x, stream);
+      dense(&sum, "residual_out", x.sizes(), rt, x);
+    }
+    if (save) {
+      const at::Tensor* t = tensor(a[6], "stats");
+      stats = t != nullptr ? *t : result(stats_shape(x), at::kFloat, x, stream);
+      dense(&stats, "stats", stats_shape(x), at::kFloat, x);
+    }
+    call("ssm_norm_fwd", nullptr, [&] {
+      return api.ssm_norm_fwd(&p, px, pr, pw, pb, po, sum.defined() ? sum.data_ptr() : nullptr,
+                              stats.defined() ? static_cast<float*>(stats.data_ptr()) : nullptr, stream);
+    });
+    const int count = 1 + sum.defined() + stats.defined();
+    if (count == 1) return wrap(out);
+    PyObject* r = PyTuple_New(count);
+    if (r == nullptr) throw Raised{};
+    int k = 0;
+    for (const at::Tensor* t : {&out, (const at::Tensor*)&sum, (const at::Tensor*)&stats})
+      if (t->defined()) PyTuple_SET_ITEM(r, k++, wrap(*t));
+    return r;
+  });
+}
+
+// norm_bwd(s, weight, dy, stats, dresidual_out, stream, outputs, rms, has_bias): fills and returns `outputs`
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) return PyErr_Format(PyExc_TypeError, "norm_bwd: 9 arguments");
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& s = first(a[0], "s");
+    const at::Tensor& dy = first(a[2], "dy");
+    const c10::cuda::CUDAGuard on(s.device());
+    io_dtype(dy);
+    const at::ScalarType io = dy.scalar_type(), rt = residual_type(s, "s", io);
+    const bool same = rt == io, bias = truth(a[8]), res = !same || a[4] != Py_None;
+    const ssm_norm_problem_t p = norm_problem(dy, rt, (truth(a[7]) ? SSM_NORM_FLAG_RMS : 0u) | (bias ? SSM_NORM_FLAG_HAS_BIAS : 0u) |
+                                                          (res ? SSM_NORM_FLAG_HAS_RESIDUAL : 0u), 0.0);
+    const int64_t D = p.D;
+    void* ps = dense(&s, "s", dy.sizes(), rt, s);
+    const float* pw = dense_float(a[1], "weight", {D}, s);
+    void* pg = dense(&dy, "dy", dy.sizes(), io, s);
+    const float* pt = dense_float(a[3], "stats", stats_shape(dy), s);
+    void* pr = dense(a[4], "dresidual_out", dy.sizes(), rt, s);
+    if (pw == nullptr) raise("weight must be a CUDA tensor");
+    if (pt == nullptr) raise("stats must be a CUDA tensor");
+    void* stream = stream_of(a[5], s);
+    PyObject* o = a[6];
+    if (same) {   // one array is the gradient of both
+      PyObject* have = PyDict_GetItemString(o, "dresidual");
+      if (have != nullptr && have != Py_None) raise("dresidual is dx where the residual has the type of the activations");
+    }
+    const at::Tensor dx = dense_output(o, "dx", dy.sizes(), io, s, stream);
+    at::Tensor dr, db;
+    if (!same) {
+      dr = dense_output(o, "dresidual", dy.sizes(), rt, s, stream);
+    } else {
+      PyObject* v = wrap(dx);
+      const int rc = PyDict_SetItemString(o, "dresidual", v);
+      Py_DECREF(v);
+      if (rc != 0) throw Raised{};
+    }
+    const at::Tensor dw = dense_output(o, "dweight", {D}, at::kFloat, s, stream);
+    if (bias) db = dense_output(o, "dbias", {D}, at::kFloat, s, stream);
+    else no_output(o, "dbias");
+    const Workspace own = workspace(api.ssm_norm_bwd_workspace_bytes(&p), s, stream);
+    auto data = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    call("ssm_norm_bwd", own.enqueue, [&] {
+      return api.ssm_norm_bwd(&p, ps, pw, pg, pt, pr, data(dx), data(dr), static_cast<float*>(data(dw)),
+                              static_cast<float*>(data(db)), data(own.buffer),
+                              own.buffer.defined() ? (size_t)own.buffer.numel() : 0, stream);
+    });
+    Py_INCREF(o);
+    return o;
+  });
+}
+
 // workspace(device index, stream) -> the cached scratch tensor or None
 PyObject* cached_workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 2) return PyErr_Format(PyExc_TypeError, "workspace: 2 arguments");
@@ -533,6 +872,8 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD("init", init),         METHOD("fwd", fwd),           METHOD("bwd", bwd),
                          METHOD("step", step),         METHOD("conv_fwd", conv_fwd), METHOD("conv_bwd", conv_bwd),
+                         METHOD("gated_fwd", gated_fwd), METHOD("gated_bwd", gated_bwd), METHOD("gated_step", gated_step),
+                         METHOD("norm_fwd", norm_fwd), METHOD("norm_bwd", norm_bwd),
                          METHOD("workspace", cached_workspace), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 
