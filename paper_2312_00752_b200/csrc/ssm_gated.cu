@@ -16,24 +16,25 @@ __device__ __forceinline__ void put(void* base, int64_t row, int64_t ld, int d, 
   static_cast<IO*>(base)[row * ld + d] = float_to_io<IO>(v);
 }
 
-// ---------------------------------------------------------------------------------------------- a thread per channel
-template <typename IO, bool DECAY>
-__global__ void __launch_bounds__(kThreads) ssm_gated_fwd_kernel(const GatedParams p) {
-  dependency_wait();
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= (int64_t)p.batch * p.D) return;
-  const int b = (int)(i / p.D), d = (int)(i % p.D);
-  const float A = DECAY ? p.A[d] : 0.f;
-  float h = p.h0 != nullptr ? p.h0[i] : 0.f;
-  for (int t = 0; t < p.L; ++t) {
-    const int64_t row = (int64_t)b * p.L + t;
-    if (p.states != nullptr && t % kGatedCkptSteps == 0) p.states[((int64_t)b * p.nck + t / kGatedCkptSteps) * p.D + d] = h;
-    const Gates k = gates<DECAY>(at<IO>(p.x, row, p.ld_x, d), at<IO>(p.gate, row, p.ld_gate, d),
-                                 DECAY ? at<IO>(p.in_gate, row, p.ld_in, d) : 0.f, A);
-    h = p.reset != nullptr && p.reset[row] ? k.u : fmaf(k.a, h, k.u);
-    if (p.y != nullptr) put<IO>(p.y, row, p.D, d, h);
+// One step, with what its gradients need: the gate g (or rho) and 1 - g, the input gate and 1 - iota, beta = sqrt(1 - a^2).
+struct Gates {
+  float a, u, g, og, iota, oi, beta, m2;
+};
+template <bool DECAY>
+__device__ __forceinline__ Gates gates(float x, float gate, float in_gate, float A) {
+  Gates r{};
+  gate_pair(gate, r.g, r.og);
+  r.a = r.og;
+  r.u = r.g * x;
+  if constexpr (DECAY) {
+    float oa;
+    decay_pair(r.g * A, r.a, oa);
+    gate_pair(in_gate, r.iota, r.oi);
+    r.m2 = oa * (2.f - oa);
+    r.beta = sqrt_approx(r.m2);
+    r.u = r.beta * r.iota * x;
   }
-  if (p.h_last != nullptr) p.h_last[i] = h;
+  return r;
 }
 
 template <typename IO, bool DECAY>
@@ -46,11 +47,11 @@ __global__ void __launch_bounds__(kThreads) ssm_gated_bwd_kernel(const GatedPara
   float carry = p.dh_last != nullptr ? p.dh_last[i] : 0.f;   // a[t+1] mu[t+1]
   float dA = 0.f;
   for (int k0 = p.nck - 1; k0 >= 0; --k0) {
-    const int t0 = k0 * kGatedCkptSteps, n = min(kGatedCkptSteps, p.L - t0);
-    float before[kGatedCkptSteps];     // the state that each step starts from
+    const int t0 = k0 * kGatedSteps, n = min(kGatedSteps, p.L - t0);
+    float before[kGatedSteps];     // the state that each step starts from
     float h = p.states[((int64_t)b * p.nck + k0) * p.D + d];
 #pragma unroll
-    for (int j = 0; j < kGatedCkptSteps; ++j) {
+    for (int j = 0; j < kGatedSteps; ++j) {
       if (j < n) {
         const int64_t row = (int64_t)b * p.L + t0 + j;
         const Gates k = gates<DECAY>(at<IO>(p.x, row, p.ld_x, d), at<IO>(p.gate, row, p.ld_gate, d),
@@ -60,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) ssm_gated_bwd_kernel(const GatedPara
       }
     }
 #pragma unroll
-    for (int j = kGatedCkptSteps - 1; j >= 0; --j) {
+    for (int j = kGatedSteps - 1; j >= 0; --j) {
       if (j < n) {
         const int64_t row = (int64_t)b * p.L + t0 + j;
         const float x = at<IO>(p.x, row, p.ld_x, d);
@@ -133,6 +134,7 @@ ssm_status_t validate(const ssm_gated_problem_t* p) {
   if (!decay(*p) && (p->ld_in_gate != 0 || p->ld_din_gate != 0)) return SSM_ERR_INVALID_ARG;
   // blocks of the grids, 32 channels of one batch entry at the least
   if ((int64_t)p->batch * (((int64_t)p->D + 31) / 32) > INT32_MAX / 16) return SSM_ERR_UNSUPPORTED;
+  if (p->L > INT32_MAX - 65536) return SSM_ERR_UNSUPPORTED;     // (steps of a round past the end)
   return SSM_OK;
 }
 
@@ -143,7 +145,7 @@ GatedParams params(const ssm_gated_problem_t& p) {
   g.batch = p.batch;
   g.L = p.L;
   g.D = p.D;
-  g.nck = (p.L + kGatedCkptSteps - 1) / kGatedCkptSteps;
+  g.nck = (p.L + kGatedSteps - 1) / kGatedSteps;
   g.ld_x = row_distance(p.ld_x, p.D);
   g.ld_gate = row_distance(p.ld_gate, p.D);
   g.ld_in = row_distance(p.ld_in_gate, p.D);
@@ -154,14 +156,10 @@ GatedParams params(const ssm_gated_problem_t& p) {
 }
 
 size_t state_bytes(const ssm_gated_problem_t& p) {
-  return (size_t)p.batch * ((p.L + kGatedCkptSteps - 1) / kGatedCkptSteps) * p.D * sizeof(float);
+  return (size_t)p.batch * ((p.L + kGatedSteps - 1) / kGatedSteps) * p.D * sizeof(float);
 }
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-template <typename IO>
-cudaError_t launch_forward(const GatedParams& p, bool dec, cudaStream_t s) {
-  return dec ? launch_channels(ssm_gated_fwd_kernel<IO, true>, p, s, p) : launch_channels(ssm_gated_fwd_kernel<IO, false>, p, s, p);
-}
 template <typename IO>
 cudaError_t launch_backward(const GatedParams& p, bool dec, cudaStream_t s) {
   return dec ? launch_channels(ssm_gated_bwd_kernel<IO, true>, p, s, p) : launch_channels(ssm_gated_bwd_kernel<IO, false>, p, s, p);
@@ -169,6 +167,16 @@ cudaError_t launch_backward(const GatedParams& p, bool dec, cudaStream_t s) {
 template <typename IO>
 cudaError_t launch_step(const GatedParams& p, float* h, bool dec, cudaStream_t s) {
   return dec ? launch_channels(ssm_gated_step_kernel<IO, true>, p, s, p, h) : launch_channels(ssm_gated_step_kernel<IO, false>, p, s, p, h);
+}
+
+// Whether pairs of channels can move as one access.
+bool wide(const ssm_gated_problem_t& p, const GatedParams& g) {
+  if ((g.D | g.ld_x | g.ld_gate | g.ld_in | g.ld_dx | g.ld_dgate | g.ld_din) % 2 != 0) return false;
+  for (const void* q : {g.x, g.gate, g.in_gate, (const void*)g.y, g.dy, (const void*)g.dx, (const void*)g.dgate, (const void*)g.din_gate})
+    if (!aligned(q, 2 * esize(p))) return false;
+  for (const float* q : {g.A, g.h0, (const float*)g.h_last, (const float*)g.states, g.dh_last, (const float*)g.dA_part, (const float*)g.dh0})
+    if (!aligned(q, 8)) return false;
+  return true;
 }
 
 ssm_status_t status(cudaError_t e) { return e == cudaSuccess ? SSM_OK : SSM_ERR_CUDA; }
@@ -207,7 +215,7 @@ ssm_status_t ssm_gated_fwd(const ssm_gated_problem_t* p, const void* x, const vo
   g.h_last = h_last;
   g.states = saved_states;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return status(p->io_dtype == SSM_BF16 ? launch_forward<__nv_bfloat16>(g, dec, s) : launch_forward<float>(g, dec, s));
+  return status(launch_gated_fwd(g, p->io_dtype, dec, wide(*p, g), s));
 }
 
 size_t ssm_gated_bwd_workspace_bytes(const ssm_gated_problem_t* p) {
@@ -246,8 +254,7 @@ ssm_status_t ssm_gated_bwd(const ssm_gated_problem_t* p, const void* x, const vo
   const bool bf16 = p->io_dtype == SSM_BF16;
   if (!saved) {
     g.states = reinterpret_cast<float*>(static_cast<char*>(workspace) + round16(dec ? (size_t)p->batch * p->D * sizeof(float) : 0));
-    const cudaError_t e = bf16 ? launch_forward<__nv_bfloat16>(g, dec, s) : launch_forward<float>(g, dec, s);
-    if (e != cudaSuccess) return SSM_ERR_CUDA;
+    if (launch_gated_fwd(g, p->io_dtype, dec, wide(*p, g), s) != cudaSuccess) return SSM_ERR_CUDA;
   }
   g.dy = dy;
   g.dh_last = dh_last;

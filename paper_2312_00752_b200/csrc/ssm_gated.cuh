@@ -1,13 +1,11 @@
-// The gates of the gated linear recurrence (include/ssm_gated.h): what a step does to the state, and what its gradients need.
+// The gates of the gated linear recurrence (include/ssm_gated.h), on one channel (float) or a pair of channels (float2, whose
+// sums and products issue two-wide), and what its kernels share.
 #pragma once
 
 #include "ssm_common.cuh"
 #include "ssm_gated.h"
 
 namespace ssm {
-
-// Steps between two saved states.
-constexpr int kGatedCkptSteps = 16;
 
 struct GatedParams {
   const void* x;
@@ -18,7 +16,7 @@ struct GatedParams {
   const float* h0;        // null: zero
   void* y;                // forward; null: not wanted (the states alone are)
   float* h_last;          // null: not wanted
-  float* states;          // [batch][nck][D] state before every kGatedCkptSteps-th step; forward: null if not wanted
+  float* states;          // [batch][nck][D] state before every kGatedSteps-th step; forward: null if not wanted
   const void* dy;         // backward
   const float* dh_last;   // null: zero
   void* dx;
@@ -28,37 +26,67 @@ struct GatedParams {
   float* dh0;             // null: not wanted
   int64_t ld_x, ld_gate, ld_in, ld_dx, ld_dgate, ld_din;   // distance of rows, in elements
   int batch, L, D, nck;
+  int tiles;              // groups of channels of one batch entry
 };
 
-// One step of one channel.  a: what is kept of the state, u: what comes in.
-//   convex: a = 1 - g.  Where g is small a is near 1 and the subtraction rounds it without bias, which matters, since the
-//   error of a multiplies over the 1 / g steps that the state remembers; where g is large 1 - g would cancel, and the
-//   quotient's other part e / (1 + e) is exact.
-//   decay: m = 1 - a = -expm1(v), v = rho A, by its series up to |v| < 1/4 (relative remainder 0.25^6 / 5040 = 5e-8), and
-//   1 - a^2 = m (2 - m) without cancellation.
-struct Gates {
-  float a, u;
-  float g, og;       // the gate (g or rho) and 1 - g
-  float iota, oi;    // decay: the input gate and 1 - iota
-  float beta;        // decay: sqrt(1 - a^2)
-  float m2;          // decay: 1 - a^2
+#ifdef __CUDACC__
+// ------------------------------------------------------------------------------------------- one channel or two
+__device__ __forceinline__ float vmul(float a, float b) { return a * b; }
+__device__ __forceinline__ float2 vmul(float2 a, float2 b) { return f2mul(a, b); }
+__device__ __forceinline__ float vadd(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 vadd(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float vfma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float2 vfma(float2 a, float2 b, float2 c) { return f2fma(a, b, c); }
+template <class F>
+__device__ __forceinline__ F vset(float v);
+template <>
+__device__ __forceinline__ float vset<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float2 vset<float2>(float v) { return make_float2(v, v); }
+template <class Op>
+__device__ __forceinline__ float vmap(float a, Op&& op) { return op(a); }
+template <class Op>
+__device__ __forceinline__ float2 vmap(float2 a, Op&& op) { return make_float2(op(a.x), op(a.y)); }
+template <class Op>
+__device__ __forceinline__ float vmap(float a, float b, float c, Op&& op) { return op(a, b, c); }
+template <class Op>
+__device__ __forceinline__ float2 vmap(float2 a, float2 b, float2 c, Op&& op) { return make_float2(op(a.x, b.x, c.x), op(a.y, b.y, c.y)); }
+
+template <class F>
+constexpr int kWidth = sizeof(F) / sizeof(float);
+
+// `F` of adjacent channels as they lie in memory
+template <typename IO, class F>
+struct Lane;
+template <>
+struct Lane<float, float> {
+  using Raw = float;
+  static __device__ __forceinline__ float open(float r) { return r; }
+  static __device__ __forceinline__ float close(float v) { return v; }
+};
+template <>
+struct Lane<float, float2> {
+  using Raw = float2;
+  static __device__ __forceinline__ float2 open(float2 r) { return r; }
+  static __device__ __forceinline__ float2 close(float2 v) { return v; }
+};
+template <>
+struct Lane<__nv_bfloat16, float> {
+  using Raw = unsigned short;
+  static __device__ __forceinline__ float open(unsigned short r) { return __uint_as_float((uint32_t)r << 16); }
+  static __device__ __forceinline__ unsigned short close(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+};
+template <>
+struct Lane<__nv_bfloat16, float2> {
+  using Raw = uint32_t;
+  static __device__ __forceinline__ float2 open(uint32_t r) { return make_float2(bf16lo(r), bf16hi(r)); }
+  static __device__ __forceinline__ uint32_t close(float2 v) {
+    const __nv_bfloat162 r = __floats2bfloat162_rn(v.x, v.y);
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
 };
 
-__device__ __forceinline__ void gate_pair(float z, float& g, float& og) {   // sigma(z) and 1 - sigma(z)
-  const float e = ex2_approx(-kLog2e * z);
-  g = rcp_approx(1.f + e);
-  og = g < 0.5f ? 1.f - g : e * g;      // (e may be infinite, then g is 0)
-}
-
-__device__ __forceinline__ float one_minus_exp(float v) {
-  float s = fmaf(v, 1.f / 720.f, 1.f / 120.f);
-  s = fmaf(v, s, 1.f / 24.f);
-  s = fmaf(v, s, 1.f / 6.f);
-  s = fmaf(v, s, 0.5f);
-  s = fmaf(v, s, 1.f);
-  return fabsf(v) < 0.25f ? -v * s : 1.f - ex2_approx(kLog2e * v);
-}
-
+// ------------------------------------------------------------------------------------------------------------- gates
 __device__ __forceinline__ float sqrt_approx(float v) {
   float r;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -70,23 +98,55 @@ __device__ __forceinline__ float rsqrt_approx(float v) {
   return r;
 }
 
-template <bool DECAY>
-__device__ __forceinline__ Gates gates(float x, float gate, float in_gate, float A) {
-  Gates r;
-  gate_pair(gate, r.g, r.og);
-  if constexpr (!DECAY) {
-    r.a = r.og;
-    r.u = r.g * x;
-  } else {
-    const float v = r.g * A;
-    const float m = one_minus_exp(v);
-    r.a = fabsf(v) < 0.25f ? 1.f - m : ex2_approx(kLog2e * v);
-    r.m2 = m * (2.f - m);
-    gate_pair(in_gate, r.iota, r.oi);
-    r.beta = sqrt_approx(r.m2);
-    r.u = r.beta * r.iota * x;
-  }
-  return r;
+// sigma(z) and 1 - sigma(z).  Where g = sigma(z) is small, 1 - g is near 1 and the subtraction rounds it without bias, which
+// matters where it is the retention, since its error multiplies over the 1 / g steps that the state remembers; where g is
+// large 1 - g would cancel, and e / (1 + e) does not (e may be infinite, then g is 0).
+template <class F>
+__device__ __forceinline__ void gate_pair(F z, F& g, F& og) {
+  const F e = vmap(vmul(z, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); });
+  g = vmap(vadd(e, vset<F>(1.f)), [](float v) { return rcp_approx(v); });
+  const F near = vfma(g, vset<F>(-1.f), vset<F>(1.f)), far = vmul(e, g);
+  og = vmap(g, near, far, [](float v, float n, float f) { return v < 0.5f ? n : f; });
 }
+
+// a = exp(v) and 1 - a for v <= 0: 1 - a = -expm1(v) by its series up to |v| < 1/4 (relative remainder 0.25^6 / 5040 = 5e-8)
+template <class F>
+__device__ __forceinline__ void decay_pair(F v, F& a, F& oa) {
+  F s = vfma(v, vset<F>(1.f / 720.f), vset<F>(1.f / 120.f));
+  s = vfma(v, s, vset<F>(1.f / 24.f));
+  s = vfma(v, s, vset<F>(1.f / 6.f));
+  s = vfma(v, s, vset<F>(0.5f));
+  s = vfma(v, s, vset<F>(1.f));
+  const F near = vmul(vmul(v, vset<F>(-1.f)), s);
+  const F ex = vmap(vmul(v, vset<F>(kLog2e)), [](float w) { return ex2_approx(w); });
+  const F far = vfma(ex, vset<F>(-1.f), vset<F>(1.f));
+  oa = vmap(v, near, far, [](float w, float n, float f) { return fabsf(w) < 0.25f ? n : f; });
+  a = vmap(v, vfma(near, vset<F>(-1.f), vset<F>(1.f)), ex, [](float w, float n, float f) { return fabsf(w) < 0.25f ? n : f; });
+}
+
+// One step of the forward recurrence: retention a and input u.
+template <bool DECAY, class F>
+__device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F& u) {
+  F g, og;
+  if constexpr (!DECAY) {
+    gate_pair(gate, g, a);
+    u = vmul(g, x);
+  } else {
+    gate_pair(gate, g, og);
+    F oa, iota, oi;
+    decay_pair(vmul(g, A), a, oa);
+    gate_pair(in_gate, iota, oi);
+    const F beta = vmap(vmul(oa, vfma(oa, vset<F>(-1.f), vset<F>(2.f))), [](float v) { return sqrt_approx(v); });   // 1 - a^2 = oa (2 - oa)
+    u = vmul(vmul(beta, iota), x);
+  }
+}
+#endif
+
+// ------------------------------------------------------------------------------------------------------------ launches
+// Steps of one warp in a tile, and between two saved states.
+constexpr int kGatedSteps = 8;
+
+// wide: pairs of channels move as one access
+cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, bool wide, cudaStream_t s);
 
 }  // namespace ssm
