@@ -169,14 +169,16 @@ cudaError_t launch_step(const GatedParams& p, float* h, bool dec, cudaStream_t s
   return dec ? launch_channels(ssm_gated_step_kernel<IO, true>, p, s, p, h) : launch_channels(ssm_gated_step_kernel<IO, false>, p, s, p, h);
 }
 
-// Whether pairs of channels can move as one access.
-bool wide(const ssm_gated_problem_t& p, const GatedParams& g) {
-  if ((g.D | g.ld_x | g.ld_gate | g.ld_in | g.ld_dx | g.ld_dgate | g.ld_din) % 2 != 0) return false;
+// The largest unit that every row begins and ends on; for bf16 pairs of channels need pairs of float32 parameters and states too.
+int unit(const ssm_gated_problem_t& p, const GatedParams& g) {
+  const size_t esz = esize(p);
+  uintptr_t bits = (uintptr_t)(g.D | g.ld_x | g.ld_gate | g.ld_in | g.ld_dx | g.ld_dgate | g.ld_din) * esz;
   for (const void* q : {g.x, g.gate, g.in_gate, (const void*)g.y, g.dy, (const void*)g.dx, (const void*)g.dgate, (const void*)g.din_gate})
-    if (!aligned(q, 2 * esize(p))) return false;
-  for (const float* q : {g.A, g.h0, (const float*)g.h_last, (const float*)g.states, g.dh_last, (const float*)g.dA_part, (const float*)g.dh0})
-    if (!aligned(q, 8)) return false;
-  return true;
+    bits |= reinterpret_cast<uintptr_t>(q);
+  if (esz == 2)
+    for (const float* q : {g.A, g.h0, (const float*)g.h_last, (const float*)g.states, g.dh_last, (const float*)g.dA_part, (const float*)g.dh0})
+      if (!aligned(q, 8)) return 2;
+  return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
 }
 
 ssm_status_t status(cudaError_t e) { return e == cudaSuccess ? SSM_OK : SSM_ERR_CUDA; }
@@ -215,7 +217,7 @@ ssm_status_t ssm_gated_fwd(const ssm_gated_problem_t* p, const void* x, const vo
   g.h_last = h_last;
   g.states = saved_states;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return status(launch_gated_fwd(g, p->io_dtype, dec, wide(*p, g), s));
+  return status(launch_gated_fwd(g, p->io_dtype, dec, unit(*p, g), s));
 }
 
 size_t ssm_gated_bwd_workspace_bytes(const ssm_gated_problem_t* p) {
@@ -254,7 +256,7 @@ ssm_status_t ssm_gated_bwd(const ssm_gated_problem_t* p, const void* x, const vo
   const bool bf16 = p->io_dtype == SSM_BF16;
   if (!saved) {
     g.states = reinterpret_cast<float*>(static_cast<char*>(workspace) + round16(dec ? (size_t)p->batch * p->D * sizeof(float) : 0));
-    if (launch_gated_fwd(g, p->io_dtype, dec, wide(*p, g), s) != cudaSuccess) return SSM_ERR_CUDA;
+    if (launch_gated_fwd(g, p->io_dtype, dec, unit(*p, g), s) != cudaSuccess) return SSM_ERR_CUDA;
   }
   g.dy = dy;
   g.dh_last = dh_last;

@@ -146,7 +146,7 @@ __device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F
 // Steps of one warp in a tile, and between two saved states.
 constexpr int kGatedSteps = 8;
 
-// wide: pairs of channels move as one access
-cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, bool wide, cudaStream_t s);
+// unit: bytes (16, 4 or, for bf16, 2) whose multiples the io pointers and the distances of rows are, D too
+cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, int unit, cudaStream_t s);
 
 }  // namespace ssm

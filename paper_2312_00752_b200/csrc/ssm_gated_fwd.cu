@@ -12,6 +12,7 @@
 // keep it infinite: it is held at the least normal number, 2^-126 of the state at most, far below its rounding.  A step that
 // resets makes P exactly zero, and zero stands for "nothing of the state passes", infinite or not.
 #include <cfloat>
+#include <type_traits>
 
 #include "ssm_gated.cuh"
 
@@ -74,74 +75,140 @@ __device__ __forceinline__ Affine<F> then(const Affine<F>& first, const Affine<F
   return r;
 }
 
-template <typename IO, class F, bool DECAY, bool RESET>
+// The inputs of a warp's steps on their way from global memory: kStages buffers of the warp's own in shared memory, filled by
+// asynchronous copies of COPY bytes (16: a row of the warp's channels is cut among its lanes; otherwise every lane copies what it
+// will read itself), or, for COPY = 0, elements too small for such copies, registers.
+constexpr int kStages = 2;
+
+__device__ __forceinline__ void copy_own(void* dst, const void* src, int bytes, std::integral_constant<int, 4>) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes) : "memory");
+}
+
+template <typename IO, class F, bool DECAY, int COPY>
+struct Feed {
+  using Raw = typename Lane<IO, F>::Raw;
+  static constexpr int kTensors = DECAY ? 3 : 2;
+  static constexpr int kRow = 32 * (int)sizeof(Raw);              // bytes of a row of the warp's channels
+  static constexpr int kBytes = COPY > 0 ? kStages * kTensors * S * kRow : 0;   // of shared memory for a warp
+
+  const IO* base[kTensors];   // this lane's first element (COPY = 16: of the chunk it copies) in the first row
+  int64_t ld[kTensors];
+  char* buf;
+  int lane, live;             // live: the lane's channels (chunk) exist
+
+  __device__ __forceinline__ void init(const GatedParams& p, int64_t row0, int d0, char* smem, int lane_) {
+    lane = lane_;
+    buf = smem;
+    const int at = COPY == 16 ? d0 + (lane * 16 % kRow) / (int)sizeof(IO) : d0 + lane * kWidth<F>;
+    live = at < p.D;
+    const int64_t c = live ? at : 0;
+    const void* const ptr[3] = {p.x, p.gate, p.in_gate};
+    const int64_t lds[3] = {p.ld_x, p.ld_gate, p.ld_in};
+#pragma unroll
+    for (int i = 0; i < kTensors; ++i) {
+      ld[i] = lds[i];
+      base[i] = static_cast<const IO*>(ptr[i]) + row0 * ld[i] + c;
+    }
+  }
+  // starts the copies of n rows (at most S) from t0 into buffer `stage`
+  __device__ __forceinline__ void issue(int t0, int n, int stage) {
+    if constexpr (COPY > 0) {
+      constexpr int kLanes = COPY == 16 ? kRow / 16 : 32;         // lanes for one row
+#pragma unroll
+      for (int i = 0; i < kTensors; ++i) {
+        char* dst = buf + (stage * kTensors + i) * S * kRow;
+#pragma unroll
+        for (int k = 0; k < S / (32 / kLanes); ++k) {
+          const int row = k * (32 / kLanes) + lane / kLanes;
+          const bool ok = live && row < n;
+          const IO* src = base[i] + (ok ? (t0 + row) * ld[i] : 0);
+          if constexpr (COPY == 16) cp_async16(dst + row * kRow + lane % kLanes * 16, src, ok);
+          else copy_own(dst + row * kRow + lane * 4, src, ok ? 4 : 0, std::integral_constant<int, 4>{});
+        }
+      }
+    }
+    if constexpr (COPY > 0) cp_async_commit();
+  }
+  __device__ __forceinline__ void arrive() {   // the older of the two buffers under way is there
+    if constexpr (COPY > 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    if constexpr (COPY == 16) __syncwarp();
+  }
+  __device__ __forceinline__ void release() {  // every lane has read its values
+    if constexpr (COPY == 16) __syncwarp();
+  }
+  __device__ __forceinline__ F get(int i, int k, int t0, int stage) const {
+    if constexpr (COPY > 0) {
+      return Lane<IO, F>::open(*reinterpret_cast<const Raw*>(buf + ((stage * kTensors + i) * S + k) * kRow + lane * (int)sizeof(Raw)));
+    } else {
+      return Lane<IO, F>::open(*reinterpret_cast<const Raw*>(base[i] + (t0 + k) * ld[i]));
+    }
+  }
+};
+
+template <typename IO, class F, bool DECAY, bool RESET, int COPY>
 __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams p) {
   using Io = Lane<IO, F>;
   using Raw = typename Io::Raw;
+  using In = Feed<IO, F, DECAY, COPY>;
   constexpr int V = kWidth<F>;
+  extern __shared__ __align__(16) char s_feed[];
   __shared__ Affine<F> s_warp[2][W][32];
   __shared__ Affine<F> s_block[2][kMaxCluster][32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int C = (int)cluster_size(), rank = (int)cluster_rank();
   const int tile = (int)(blockIdx.x / (unsigned)C);
   const int b = tile / p.tiles;
-  const int d = ((tile - b * p.tiles) * 32 + lane) * V;
+  const int d0 = (tile - b * p.tiles) * 32 * V, d = d0 + lane * V;
   const bool live = d < p.D;
-  const int dc = live ? d : 0;                       // (lanes past the last channel run along on the first)
   const int64_t row0 = (int64_t)b * p.L;
+  const int rounds = (p.L + kTile * C - 1) / (kTile * C);
+  const int step = kTile * C;                        // from a tile to the next one of this block
+  int t0 = (rank * W + w) * S;                       // this warp's first step in the round
+  In in;
+  in.init(p, row0, d0, s_feed + w * In::kBytes, lane);
   dependency_wait();
 
-  const IO* __restrict__ px = static_cast<const IO*>(p.x) + row0 * p.ld_x + dc;
-  const IO* __restrict__ pg = static_cast<const IO*>(p.gate) + row0 * p.ld_gate + dc;
-  const IO* __restrict__ pi = DECAY ? static_cast<const IO*>(p.in_gate) + row0 * p.ld_in + dc : nullptr;
+  in.issue(t0, p.L - t0, 0);
+  in.issue(t0 + step, p.L - t0 - step, 1);
+  // bytes of the mask: those of the step after the next are loaded where those of this one are looked at
   const uint8_t* __restrict__ pr = RESET ? p.reset + row0 : nullptr;
-  IO* __restrict__ py = static_cast<IO*>(p.y) + row0 * p.D + dc;
-  F A = vset<F>(0.f);
-  if constexpr (DECAY) A = *reinterpret_cast<const F*>(p.A + dc);
-  F carry = vset<F>(0.f);                            // the state that enters the round
-  if (p.h0 != nullptr) carry = *reinterpret_cast<const F*>(p.h0 + (int64_t)b * p.D + dc);
+  auto mask_at = [&](int t) -> unsigned { return RESET && lane < S && t + lane < p.L ? pr[t + lane] : 0u; };
+  unsigned mask0 = mask_at(t0), mask1 = mask_at(t0 + step);
+  F A = vset<F>(0.f), carry = vset<F>(0.f);          // carry: the state that enters the round
+  if (live) {
+    if constexpr (DECAY) A = *reinterpret_cast<const F*>(p.A + d);
+    if (p.h0 != nullptr) carry = *reinterpret_cast<const F*>(p.h0 + (int64_t)b * p.D + d);
+  }
 
-  Raw rx[S], rg[S], ri[DECAY ? S : 1];
-  unsigned cut = 0;                                  // bit u: step u of this warp resets
-  auto fetch = [&](int t0) {
-    const int n = min(S, p.L - t0);
-    if (n <= 0) return;
-    const IO *qx = px + t0 * p.ld_x, *qg = pg + t0 * p.ld_gate, *qi = DECAY ? pi + t0 * p.ld_in : nullptr;
-#pragma unroll
-    for (int u = 0; u < S; ++u) {
-      if (u < n) {
-        rx[u] = *reinterpret_cast<const Raw*>(qx + u * p.ld_x);
-        rg[u] = *reinterpret_cast<const Raw*>(qg + u * p.ld_gate);
-        if constexpr (DECAY) ri[u] = *reinterpret_cast<const Raw*>(qi + u * p.ld_in);
-      }
-    }
-    if constexpr (RESET) cut = __ballot_sync(~0u, lane < n && pr[t0 + min(lane, n - 1)] != 0);
-  };
-
-  const int rounds = (p.L + kTile * C - 1) / (kTile * C);
-  fetch((rank * W + w) * S);
-  for (int r = 0; r < rounds; ++r) {
-    const int t0 = ((r * C + rank) * W + w) * S;
-    const int n = min(S, p.L - t0);                  // steps of this warp (not above zero: none)
+  for (int r = 0; r < rounds; ++r, t0 += step) {
+    const int n = p.L - t0;                          // steps left from this warp's first one on (S or more: all of its)
+    const int half = r & 1;
     F a[S], u[S];
     Affine<F> mine{vset<F>(1.f), vset<F>(0.f)};
-    const unsigned cuts = RESET ? cut : 0u;
+    const unsigned cuts = RESET ? __ballot_sync(~0u, mask0 != 0) : 0u;   // bit k: step k of this warp resets
+    mask0 = mask1;
+    mask1 = mask_at(t0 + 2 * step);
+    in.arrive();
+    auto read = [&](auto all) {
 #pragma unroll
-    for (int k = 0; k < S; ++k) {
-      if (k < n) {
-        step_inputs<DECAY>(Io::open(rx[k]), Io::open(rg[k]), DECAY ? Io::open(ri[DECAY ? k : 0]) : vset<F>(0.f), A, a[k], u[k]);
-        if (RESET && (cuts >> k & 1)) {
-          mine = {vset<F>(0.f), u[k]};
-        } else {
-          mine.S = vfma(a[k], mine.S, u[k]);
-          mine.P = vmul(a[k], mine.P);
+      for (int k = 0; k < S; ++k) {
+        if (decltype(all)::value || k < n) {
+          step_inputs<DECAY>(in.get(0, k, t0, half), in.get(1, k, t0, half), DECAY ? in.get(DECAY ? 2 : 0, k, t0, half) : vset<F>(0.f), A, a[k], u[k]);
+          if (RESET && (cuts >> k & 1)) {
+            mine = {vset<F>(0.f), u[k]};
+          } else {
+            mine.S = vfma(a[k], mine.S, u[k]);
+            mine.P = vmul(a[k], mine.P);
+          }
         }
       }
-    }
+    };
+    if (n >= S) read(std::true_type{});
+    else if (n > 0) read(std::false_type{});
+    in.release();
+    in.issue(t0 + 2 * step, n - 2 * step, half);
     if (!RESET || cuts == 0) mine.P = vmap(mine.P, [](float v) { return fmaxf(v, FLT_MIN); });
-    if (r + 1 < rounds) fetch(t0 + kTile * C);
 
-    const int half = r & 1;
     s_warp[half][w][lane] = mine;
     __syncthreads();
     F h;
@@ -165,25 +232,30 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
         remote_store(to + sizeof(F), all.S);
       }
       cluster_sync();
-      F in = carry;
+      F enter = carry;
       for (int j = 0; j < C; ++j) {
-        if (j == rank) in = carry;
+        if (j == rank) enter = carry;
         carry = apply<RESET>(s_block[half][j][lane], carry);
       }
-      h = w == 0 ? in : apply<RESET>(before, in);
+      h = w == 0 ? enter : apply<RESET>(before, enter);
     }
 
     if (live && n > 0) {
       if (p.states != nullptr) *reinterpret_cast<F*>(p.states + ((int64_t)b * p.nck + t0 / S) * p.D + d) = h;
-      IO* __restrict__ qy = py + (int64_t)t0 * p.D;
       if (p.y != nullptr) {
+        IO* __restrict__ py = static_cast<IO*>(p.y) + (row0 + t0) * p.D + d;
+        auto write = [&](auto all) {
 #pragma unroll
-        for (int k = 0; k < S; ++k) {
-          if (k < n) {
-            h = RESET && (cuts >> k & 1) ? u[k] : vfma(a[k], h, u[k]);
-            *reinterpret_cast<Raw*>(qy + (int64_t)k * p.D) = Io::close(h);
+          for (int k = 0; k < S; ++k) {
+            if (decltype(all)::value || k < n) {
+              h = RESET && (cuts >> k & 1) ? u[k] : vfma(a[k], h, u[k]);
+              *reinterpret_cast<Raw*>(py) = Io::close(h);
+              py += p.D;
+            }
           }
-        }
+        };
+        if (n >= S) write(std::true_type{});
+        else write(std::false_type{});
       }
     }
   }
@@ -205,29 +277,35 @@ int choose_cluster(long long tiles, int L, long long resident) {
   return best;
 }
 
-template <typename IO, class F, bool DECAY, bool RESET>
+template <typename IO, class F, bool DECAY, bool RESET, int COPY>
 cudaError_t launch(GatedParams p, cudaStream_t s) {
-  const auto kernel = ssm_gated_fwd_kernel<IO, F, DECAY, RESET>;
+  const auto kernel = ssm_gated_fwd_kernel<IO, F, DECAY, RESET, COPY>;
+  constexpr size_t smem = (size_t)W * Feed<IO, F, DECAY, COPY>::kBytes;
   p.tiles = (p.D + 32 * kWidth<F> - 1) / (32 * kWidth<F>);
   KernelLimits lim;
-  const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), 32 * W, 0, &lim);
+  const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), 32 * W, smem, &lim);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.tiles * p.batch;
   const int c = choose_cluster(tiles, p.L, (long long)lim.sms * lim.per_sm);
-  return launch_dependent(kernel, (unsigned)(tiles * c), 32 * W, 0, c, s, p);
+  return launch_dependent(kernel, (unsigned)(tiles * c), 32 * W, smem, c, s, p);
 }
 
-template <typename IO, class F>
+template <typename IO, class F, int COPY>
 cudaError_t launch_form(const GatedParams& p, bool decay, cudaStream_t s) {
-  if (p.reset != nullptr) return decay ? launch<IO, F, true, true>(p, s) : launch<IO, F, false, true>(p, s);
-  return decay ? launch<IO, F, true, false>(p, s) : launch<IO, F, false, false>(p, s);
+  if (p.reset != nullptr) return decay ? launch<IO, F, true, true, COPY>(p, s) : launch<IO, F, false, true, COPY>(p, s);
+  return decay ? launch<IO, F, true, false, COPY>(p, s) : launch<IO, F, false, false, COPY>(p, s);
 }
 
 }  // namespace
 
-cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, bool wide, cudaStream_t s) {
-  if (io_dtype == SSM_BF16) return wide ? launch_form<__nv_bfloat16, float2>(p, decay, s) : launch_form<__nv_bfloat16, float>(p, decay, s);
-  return wide ? launch_form<float, float2>(p, decay, s) : launch_form<float, float>(p, decay, s);
+// Pairs of bf16 channels per lane (a row of a warp is a 128-byte line either way); float32 io has twice the bytes for the same
+// arithmetic and does without packed instructions.
+cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, int unit, cudaStream_t s) {
+  if (io_dtype == SSM_BF16) {
+    if (unit == 16) return launch_form<__nv_bfloat16, float2, 16>(p, decay, s);
+    return unit >= 4 ? launch_form<__nv_bfloat16, float2, 4>(p, decay, s) : launch_form<__nv_bfloat16, float, 0>(p, decay, s);
+  }
+  return unit == 16 ? launch_form<float, float, 16>(p, decay, s) : launch_form<float, float, 4>(p, decay, s);
 }
 
 }  // namespace ssm
