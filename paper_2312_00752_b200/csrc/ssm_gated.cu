@@ -18,7 +18,7 @@ __device__ __forceinline__ void put(void* base, int64_t row, int64_t ld, int d, 
 
 // One step, with what its gradients need: the gate g (or rho) and 1 - g, the input gate and 1 - iota, beta = sqrt(1 - a^2).
 struct Gates {
-  float a, u, g, og, iota, oi, beta, m2;
+  float a, u, g, og, iota, oi, beta, inv;
 };
 template <bool DECAY>
 __device__ __forceinline__ Gates gates(float x, float gate, float in_gate, float A) {
@@ -30,8 +30,7 @@ __device__ __forceinline__ Gates gates(float x, float gate, float in_gate, float
     float oa;
     decay_pair(r.g * A, r.a, oa);
     gate_pair(in_gate, r.iota, r.oi);
-    r.m2 = oa * (2.f - oa);
-    r.beta = sqrt_approx(r.m2);
+    input_scale(oa, r.beta, r.inv);
     r.u = r.beta * r.iota * x;
   }
   return r;
@@ -68,8 +67,7 @@ __global__ void __launch_bounds__(kThreads) ssm_gated_bwd_kernel(const GatedPara
         const Gates k = gates<DECAY>(x, at<IO>(p.gate, row, p.ld_gate, d), DECAY ? at<IO>(p.in_gate, row, p.ld_in, d) : 0.f, A);
         const float mu = at<IO>(p.dy, row, p.D, d) + carry;
         if constexpr (DECAY) {
-          const float rs = k.m2 == 0.f ? 0.f : rsqrt_approx(k.m2);     // (1 - a^2 = 0: rho is 0, and so are its gradients)
-          const float m = mu * k.a * fmaf(-k.a * k.iota, x * rs, before[j]);
+          const float m = mu * k.a * fmaf(-k.a * k.iota, x * k.inv, before[j]);
           put<IO>(p.dx, row, p.ld_dx, d, mu * k.beta * k.iota);
           put<IO>(p.din_gate, row, p.ld_din, d, mu * k.u * k.oi);
           put<IO>(p.dgate, row, p.ld_dgate, d, m * A * k.g * k.og);

@@ -55,6 +55,14 @@ __device__ __forceinline__ float2 vmap(float2 a, float2 b, float2 c, Op&& op) { 
 template <class F>
 constexpr int kWidth = sizeof(F) / sizeof(float);
 
+// Gates of bf16 io come no lower than this in the decay form (sigma: 1e-19), see gate_two.
+constexpr float kGateFloor = -43.5f;
+__device__ __forceinline__ float floor_gate(float z) {   // (NaN stays)
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(kGateFloor));
+  return r;
+}
+
 // `F` of adjacent channels as they lie in memory
 template <typename IO, class F>
 struct Lane;
@@ -74,12 +82,18 @@ template <>
 struct Lane<__nv_bfloat16, float> {
   using Raw = unsigned short;
   static __device__ __forceinline__ float open(unsigned short r) { return __uint_as_float((uint32_t)r << 16); }
+  static __device__ __forceinline__ float open_gate(unsigned short r) { return floor_gate(open(r)); }
   static __device__ __forceinline__ unsigned short close(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 };
 template <>
 struct Lane<__nv_bfloat16, float2> {
   using Raw = uint32_t;
   static __device__ __forceinline__ float2 open(uint32_t r) { return make_float2(bf16lo(r), bf16hi(r)); }
+  static __device__ __forceinline__ float2 open_gate(uint32_t r) {   // max(gate, kGateFloor), both at once (NaN stays)
+    uint32_t v;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(r), "r"(0xc22ec22eu));
+    return open(v);
+  }
   static __device__ __forceinline__ uint32_t close(float2 v) {
     const __nv_bfloat162 r = __floats2bfloat162_rn(v.x, v.y);
     return *reinterpret_cast<const uint32_t*>(&r);
@@ -87,11 +101,6 @@ struct Lane<__nv_bfloat16, float2> {
 };
 
 // ------------------------------------------------------------------------------------------------------------- gates
-__device__ __forceinline__ float sqrt_approx(float v) {
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 __device__ __forceinline__ float rsqrt_approx(float v) {
   float r;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -124,19 +133,57 @@ __device__ __forceinline__ void decay_pair(F v, F& a, F& oa) {
   a = vmap(v, vfma(near, vset<F>(-1.f), vset<F>(1.f)), ex, [](float w, float n, float f) { return fabsf(w) < 0.25f ? n : f; });
 }
 
-// One step of the forward recurrence: retention a and input u.
-template <bool DECAY, class F>
+// The same for -1 <= A <= 0, with w = -v in [0, 1]: (1 - exp(-w)) / w by its Chebyshev interpolation of degree 6 (relative error
+// 3e-9), no special-function operation and no case distinction.
+template <class F>
+__device__ __forceinline__ void decay_pair_small(F w, F& a, F& oa) {
+  F s = vfma(w, vset<F>(1.29076311e-4f), vset<F>(-1.30077498e-3f));
+  s = vfma(w, s, vset<F>(8.27550516e-3f));
+  s = vfma(w, s, vset<F>(-4.16468494e-2f));
+  s = vfma(w, s, vset<F>(1.66663408e-1f));
+  s = vfma(w, s, vset<F>(-4.99999791e-1f));
+  s = vfma(w, s, vset<F>(1.f));
+  oa = vmul(w, s);
+  a = vfma(oa, vset<F>(-1.f), vset<F>(1.f));
+}
+
+// sigma of two gates with one reciprocal, 1 / ((1 + e1) (1 + e2)): the special-function unit, four lanes a cycle, is what limits
+// bf16 io next to the memory.  The gates come no lower than kGateFloor, so that the product stays in range.
+template <class F>
+__device__ __forceinline__ void gate_two(F z1, F z2, F& g1, F& g2) {
+  const F d1 = vadd(vmap(vmul(z1, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f));
+  const F d2 = vadd(vmap(vmul(z2, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f));
+  const F r = vmap(vmul(d1, d2), [](float v) { return rcp_approx(v); });
+  g1 = vmul(r, d2);
+  g2 = vmul(r, d1);
+}
+// sqrt(1 - a^2) = sqrt(oa (2 - oa)) and its reciprocal, which is 0 where a = 1
+template <class F>
+__device__ __forceinline__ void input_scale(F oa, F& beta, F& inv) {
+  const F m2 = vmul(oa, vfma(oa, vset<F>(-1.f), vset<F>(2.f)));
+  inv = vmap(m2, [](float v) { return rsqrt_approx(fmaxf(v, 1e-37f)); });   // (1 / beta meets rho, which is 0 there, or so near)
+  beta = vmul(m2, inv);
+}
+
+// One step of the forward recurrence: retention a and input u.  PAIRED: the gates share a reciprocal; SMALL: -1 <= A <= 0, and A
+// comes negated.
+template <bool DECAY, bool PAIRED, bool SMALL, class F>
 __device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F& u) {
   F g, og;
   if constexpr (!DECAY) {
     gate_pair(gate, g, a);
     u = vmul(g, x);
   } else {
-    gate_pair(gate, g, og);
-    F oa, iota, oi;
-    decay_pair(vmul(g, A), a, oa);
-    gate_pair(in_gate, iota, oi);
-    const F beta = vmap(vmul(oa, vfma(oa, vset<F>(-1.f), vset<F>(2.f))), [](float v) { return sqrt_approx(v); });   // 1 - a^2 = oa (2 - oa)
+    F oa, iota, oi, beta, inv;
+    if constexpr (PAIRED) {
+      gate_two(gate, in_gate, g, iota);
+    } else {
+      gate_pair(gate, g, og);
+      gate_pair(in_gate, iota, oi);
+    }
+    if constexpr (SMALL) decay_pair_small(vmul(g, A), a, oa);
+    else decay_pair(vmul(g, A), a, oa);
+    input_scale(oa, beta, inv);
     u = vmul(vmul(beta, iota), x);
   }
 }
@@ -144,7 +191,7 @@ __device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F
 
 // ------------------------------------------------------------------------------------------------------------ launches
 // Steps of one warp in a tile, and between two saved states.
-constexpr int kGatedSteps = 8;
+constexpr int kGatedSteps = 16;
 
 // unit: bytes (16, 4 or, for bf16, 2) whose multiples the io pointers and the distances of rows are, D too
 cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, int unit, cudaStream_t s);

@@ -12,6 +12,7 @@
 // keep it infinite: it is held at the least normal number, 2^-126 of the state at most, far below its rounding.  A step that
 // resets makes P exactly zero, and zero stands for "nothing of the state passes", infinite or not.
 #include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 #include "ssm_gated.cuh"
@@ -21,38 +22,12 @@ namespace ssm {
 namespace {
 
 constexpr int S = kGatedSteps;
-constexpr int W = 8;                 // warps of a block
+constexpr int W = 4;                 // warps of a block
 constexpr int kTile = S * W;         // steps of a tile
 constexpr int kMaxCluster = 8;
 
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ unsigned cluster_size() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// stores to the same place in the shared memory of block `rank` of the cluster
-__device__ __forceinline__ unsigned remote_address(const void* local, unsigned rank) {
-  unsigned r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((unsigned)__cvta_generic_to_shared(local)), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void remote_store(unsigned address, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(address), "f"(v) : "memory");
-}
-__device__ __forceinline__ void remote_store(unsigned address, float2 v) {
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(address), "f"(v.x), "f"(v.y) : "memory");
-}
-
 template <class F>
-struct Affine {
+struct alignas(2 * sizeof(F)) Affine {
   F P, S;
 };
 
@@ -75,85 +50,148 @@ __device__ __forceinline__ Affine<F> then(const Affine<F>& first, const Affine<F
   return r;
 }
 
-// The inputs of a warp's steps on their way from global memory: kStages buffers of the warp's own in shared memory, filled by
-// asynchronous copies of COPY bytes (16: a row of the warp's channels is cut among its lanes; otherwise every lane copies what it
-// will read itself), or, for COPY = 0, elements too small for such copies, registers.
-constexpr int kStages = 2;
+// --------------------------------------------------------------------------------------- between the blocks of a cluster
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ unsigned cluster_size() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned shared_address(const void* q) { return (unsigned)__cvta_generic_to_shared(q); }
+__device__ __forceinline__ unsigned remote_address(const void* local, unsigned rank) {   // the same place in block `rank`
+  unsigned r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(shared_address(local)), "r"(rank));
+  return r;
+}
+// A store into another block's shared memory that counts its bytes at a barrier there: the reader waits for the bytes, and the
+// writer for nothing.  (A barrier of the whole cluster with its release waits for every store of y under way and every copy: 1.5
+// of the 9.6 cycles between two instructions of a warp.)
+__device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine<float>& v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.P), "f"(v.S), "r"(barrier) : "memory");
+}
+__device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine<float2>& v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "f"(v.P.x), "f"(v.P.y),
+               "f"(v.S.x), "f"(v.S.y), "r"(barrier)
+               : "memory");
+}
+__device__ __forceinline__ void barrier_init(const void* barrier) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(barrier)) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(const void* barrier, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
+}
+// Waits for the bytes of a phase.  The blocks of a cluster run at the same time and send before they wait, so that every wait
+// ends; the limit (seconds) keeps a fault elsewhere from holding the GPU.  False: it was reached.
+constexpr int kWaitLimit = 1 << 20;
+__device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase) {
+  for (int i = 0; i < kWaitLimit; ++i) {
+    unsigned done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(shared_address(barrier)), "r"(phase)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
+}
 
-__device__ __forceinline__ void copy_own(void* dst, const void* src, int bytes, std::integral_constant<int, 4>) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes) : "memory");
+// The inputs of a warp's steps on their way from global memory: kAhead tiles ahead, through buffers of the warp's own in shared
+// memory that asynchronous copies of COPY bytes fill (16: a row of the warp's channels is cut among its lanes; 4: every
+// lane copies what it will read itself), or, for COPY = 0, elements too small for such copies, one tile ahead through registers.
+__device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
 }
 
 template <typename IO, class F, bool DECAY, int COPY>
 struct Feed {
   using Raw = typename Lane<IO, F>::Raw;
+  static constexpr int kAhead = COPY > 0 ? 2 : 1;
   static constexpr int kTensors = DECAY ? 3 : 2;
-  static constexpr int kRow = 32 * (int)sizeof(Raw);              // bytes of a row of the warp's channels
-  static constexpr int kBytes = COPY > 0 ? kStages * kTensors * S * kRow : 0;   // of shared memory for a warp
+  static constexpr int kRow = 32 * (int)sizeof(Raw);                          // bytes of a row of the warp's channels
+  static constexpr int kBytes = COPY > 0 ? kAhead * kTensors * S * kRow : 0;  // of shared memory for a warp
+  static constexpr int kLanes = COPY == 16 ? kRow / 16 : 32;                  // lanes that copy a row
+  static constexpr int kRows = 32 / kLanes;                                   // rows that the warp copies at once
 
-  const IO* base[kTensors];   // this lane's first element (COPY = 16: of the chunk it copies) in the first row
-  int64_t ld[kTensors];
+  const char* next[kTensors];   // this lane's first element (or chunk) in its first row of the next tile to fetch
+  int64_t ld[kTensors];         // bytes
   char* buf;
-  int lane, live;             // live: the lane's channels (chunk) exist
+  int lane;
+  bool live;                    // the lane's channels (or chunk) exist
+  Raw raw[COPY > 0 ? 1 : kTensors][COPY > 0 ? 1 : S];
 
-  __device__ __forceinline__ void init(const GatedParams& p, int64_t row0, int d0, char* smem, int lane_) {
+  __device__ __forceinline__ void init(const GatedParams& p, int64_t row, int d0, char* smem, int lane_) {
     lane = lane_;
     buf = smem;
-    const int at = COPY == 16 ? d0 + (lane * 16 % kRow) / (int)sizeof(IO) : d0 + lane * kWidth<F>;
+    const int at = d0 + (COPY == 16 ? lane % kLanes * (16 / (int)sizeof(IO)) : lane * kWidth<F>);
     live = at < p.D;
-    const int64_t c = live ? at : 0;
     const void* const ptr[3] = {p.x, p.gate, p.in_gate};
     const int64_t lds[3] = {p.ld_x, p.ld_gate, p.ld_in};
 #pragma unroll
     for (int i = 0; i < kTensors; ++i) {
-      ld[i] = lds[i];
-      base[i] = static_cast<const IO*>(ptr[i]) + row0 * ld[i] + c;
+      ld[i] = lds[i] * (int)sizeof(IO);
+      next[i] = static_cast<const char*>(ptr[i]) + (row + lane / kLanes) * ld[i] + (live ? at : 0) * (int)sizeof(IO);
     }
   }
-  // starts the copies of n rows (at most S) from t0 into buffer `stage`
-  __device__ __forceinline__ void issue(int t0, int n, int stage) {
-    if constexpr (COPY > 0) {
-      constexpr int kLanes = COPY == 16 ? kRow / 16 : 32;         // lanes for one row
+  // fetches the next tile's rows, n of them (S at most), and moves on by `step` rows
+  template <bool ALL>
+  __device__ __forceinline__ void rows(int n, int stage) {
 #pragma unroll
-      for (int i = 0; i < kTensors; ++i) {
-        char* dst = buf + (stage * kTensors + i) * S * kRow;
-#pragma unroll
-        for (int k = 0; k < S / (32 / kLanes); ++k) {
-          const int row = k * (32 / kLanes) + lane / kLanes;
-          const bool ok = live && row < n;
-          const IO* src = base[i] + (ok ? (t0 + row) * ld[i] : 0);
-          if constexpr (COPY == 16) cp_async16(dst + row * kRow + lane % kLanes * 16, src, ok);
-          else copy_own(dst + row * kRow + lane * 4, src, ok ? 4 : 0, std::integral_constant<int, 4>{});
+    for (int i = 0; i < kTensors; ++i) {
+      const char* src = next[i];
+#pragma unroll(COPY == 4 ? 4 : S / kRows)
+      for (int k = 0; k < S / kRows; ++k, src += kRows * ld[i]) {
+        const int row = k * kRows + lane / kLanes;
+        if constexpr (COPY > 0) {
+          char* dst = buf + ((stage * kTensors + i) * S + row) * kRow + lane % kLanes * COPY;
+          const bool ok = live && (ALL || row < n);
+          const char* from = ALL || row < n ? src : next[i];     // (n > 0, but this lane's first row may be past it)
+          if constexpr (COPY == 16) cp_async16(dst, from, ok);
+          else cp_async4(dst, from, ok);
+        } else if (ALL || row < n) {
+          raw[i][k] = *reinterpret_cast<const Raw*>(src);
         }
       }
     }
-    if constexpr (COPY > 0) cp_async_commit();
   }
-  __device__ __forceinline__ void arrive() {   // the older of the two buffers under way is there
+  __device__ __forceinline__ void issue(int n, int stage, int step) {
+    if (n >= S) rows<true>(n, stage);
+    else if (n > 0) rows<false>(n, stage);
+    if constexpr (COPY > 0) cp_async_commit();
+#pragma unroll
+    for (int i = 0; i < kTensors; ++i) next[i] += step * ld[i];
+  }
+  __device__ __forceinline__ void arrive() {   // the oldest tile under way is there
     if constexpr (COPY > 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
     if constexpr (COPY == 16) __syncwarp();
   }
   __device__ __forceinline__ void release() {  // every lane has read its values
     if constexpr (COPY == 16) __syncwarp();
   }
-  __device__ __forceinline__ F get(int i, int k, int t0, int stage) const {
-    if constexpr (COPY > 0) {
-      return Lane<IO, F>::open(*reinterpret_cast<const Raw*>(buf + ((stage * kTensors + i) * S + k) * kRow + lane * (int)sizeof(Raw)));
-    } else {
-      return Lane<IO, F>::open(*reinterpret_cast<const Raw*>(base[i] + (t0 + k) * ld[i]));
-    }
+  __device__ __forceinline__ Raw get(int i, int k, int stage) const {
+    if constexpr (COPY > 0) return *reinterpret_cast<const Raw*>(buf + ((stage * kTensors + i) * S + k) * kRow + lane * (int)sizeof(Raw));
+    else return raw[i][k];
   }
 };
 
 template <typename IO, class F, bool DECAY, bool RESET, int COPY>
-__global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams p) {
+__global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedParams p) {
   using Io = Lane<IO, F>;
   using Raw = typename Io::Raw;
   using In = Feed<IO, F, DECAY, COPY>;
-  constexpr int V = kWidth<F>;
+  constexpr int V = kWidth<F>, kAhead = In::kAhead;
+  constexpr bool PAIRED = sizeof(IO) == 2;
   extern __shared__ __align__(16) char s_feed[];
   __shared__ Affine<F> s_warp[2][W][32];
   __shared__ Affine<F> s_block[2][kMaxCluster][32];
+  __shared__ uint64_t s_there[2];                    // one barrier for each half of s_block
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int C = (int)cluster_size(), rank = (int)cluster_rank();
   const int tile = (int)(blockIdx.x / (unsigned)C);
@@ -164,13 +202,20 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
   const int rounds = (p.L + kTile * C - 1) / (kTile * C);
   const int step = kTile * C;                        // from a tile to the next one of this block
   int t0 = (rank * W + w) * S;                       // this warp's first step in the round
+  if (C > 1) {
+    if (threadIdx.x == 0) {
+      barrier_init(&s_there[0]);
+      barrier_init(&s_there[1]);
+    }
+    cluster_sync();                                  // (every block is there, its barriers set up)
+  }
   In in;
-  in.init(p, row0, d0, s_feed + w * In::kBytes, lane);
+  in.init(p, row0 + t0, d0, s_feed + w * In::kBytes, lane);
   dependency_wait();
 
-  in.issue(t0, p.L - t0, 0);
-  in.issue(t0 + step, p.L - t0 - step, 1);
-  // bytes of the mask: those of the step after the next are loaded where those of this one are looked at
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) in.issue(p.L - t0 - i * step, i, step);
+  // bytes of the mask: those of the tile after the next are loaded where those of this one are looked at
   const uint8_t* __restrict__ pr = RESET ? p.reset + row0 : nullptr;
   auto mask_at = [&](int t) -> unsigned { return RESET && lane < S && t + lane < p.L ? pr[t + lane] : 0u; };
   unsigned mask0 = mask_at(t0), mask1 = mask_at(t0 + step);
@@ -178,6 +223,12 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
   if (live) {
     if constexpr (DECAY) A = *reinterpret_cast<const F*>(p.A + d);
     if (p.h0 != nullptr) carry = *reinterpret_cast<const F*>(p.h0 + (int64_t)b * p.D + d);
+  }
+  bool small = false;                                // -1 <= A <= 0 in all of the warp's channels
+  if constexpr (DECAY) {
+    bool mine = true;
+    vmap(A, [&](float v) { mine = mine && v >= -1.f && v <= 0.f; return v; });
+    small = __all_sync(~0u, mine);
   }
 
   for (int r = 0; r < rounds; ++r, t0 += step) {
@@ -189,11 +240,16 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
     mask0 = mask1;
     mask1 = mask_at(t0 + 2 * step);
     in.arrive();
-    auto read = [&](auto all) {
+    auto read = [&](auto all_steps, auto small_A) {
+      constexpr bool SMALL = decltype(small_A)::value;
+      const F At = SMALL ? vmul(A, vset<F>(-1.f)) : A;
 #pragma unroll
       for (int k = 0; k < S; ++k) {
-        if (decltype(all)::value || k < n) {
-          step_inputs<DECAY>(in.get(0, k, t0, half), in.get(1, k, t0, half), DECAY ? in.get(DECAY ? 2 : 0, k, t0, half) : vset<F>(0.f), A, a[k], u[k]);
+        if (decltype(all_steps)::value || k < n) {
+          const F x = Io::open(in.get(0, k, half));
+          if constexpr (!DECAY) step_inputs<false, false, false>(x, Io::open(in.get(1, k, half)), x, x, a[k], u[k]);
+          else if constexpr (PAIRED) step_inputs<true, true, SMALL>(x, Io::open_gate(in.get(1, k, half)), Io::open_gate(in.get(2, k, half)), At, a[k], u[k]);
+          else step_inputs<true, false, SMALL>(x, Io::open(in.get(1, k, half)), Io::open(in.get(2, k, half)), At, a[k], u[k]);
           if (RESET && (cuts >> k & 1)) {
             mine = {vset<F>(0.f), u[k]};
           } else {
@@ -203,13 +259,21 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
         }
       }
     };
-    if (n >= S) read(std::true_type{});
-    else if (n > 0) read(std::false_type{});
+    using Yes = std::true_type;
+    using No = std::false_type;
+    if (n >= S) {
+      if (DECAY && small) read(Yes{}, Yes{});
+      else read(Yes{}, No{});
+    } else if (n > 0) {
+      if (DECAY && small) read(No{}, Yes{});
+      else read(No{}, No{});
+    }
     in.release();
-    in.issue(t0 + 2 * step, n - 2 * step, half);
+    in.issue(n - kAhead * step, kAhead == 2 ? half : 0, step);
     if (!RESET || cuts == 0) mine.P = vmap(mine.P, [](float v) { return fmaxf(v, FLT_MIN); });
 
     s_warp[half][w][lane] = mine;
+    if (C > 1 && threadIdx.x == 0) barrier_expect(&s_there[half], C * 32 * sizeof(Affine<F>));
     __syncthreads();
     F h;
     if (C == 1) {
@@ -220,18 +284,16 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
         carry = apply<RESET>(s_warp[half][j][lane], carry);
       }
     } else {
-      Affine<F> before{vset<F>(1.f), vset<F>(0.f)}, all = s_warp[half][0][lane];
+      Affine<F> before{vset<F>(1.f), vset<F>(0.f)};
+      if (w > 0) before = s_warp[half][0][lane];
 #pragma unroll
-      for (int j = 1; j < W; ++j) {
-        if (j == w) before = all;
-        all = then<RESET>(all, s_warp[half][j][lane]);
+      for (int j = 1; j < W - 1; ++j)
+        if (j < w) before = then<RESET>(before, s_warp[half][j][lane]);
+      if (w == W - 1) {
+        const Affine<F> all = then<RESET>(before, mine);
+        for (int j = 0; j < C; ++j) send(remote_address(&s_block[half][rank][lane], j), remote_address(&s_there[half], j), all);
       }
-      if (w < C) {                                   // warp w tells block w
-        const unsigned to = remote_address(&s_block[half][rank][lane], w);
-        remote_store(to, all.P);
-        remote_store(to + sizeof(F), all.S);
-      }
-      cluster_sync();
+      if (!barrier_wait(&s_there[half], r >> 1 & 1)) carry = vset<F>(NAN);
       F enter = carry;
       for (int j = 0; j < C; ++j) {
         if (j == rank) enter = carry;
@@ -244,18 +306,18 @@ __global__ void __launch_bounds__(32 * W) ssm_gated_fwd_kernel(const GatedParams
       if (p.states != nullptr) *reinterpret_cast<F*>(p.states + ((int64_t)b * p.nck + t0 / S) * p.D + d) = h;
       if (p.y != nullptr) {
         IO* __restrict__ py = static_cast<IO*>(p.y) + (row0 + t0) * p.D + d;
-        auto write = [&](auto all) {
+        auto write = [&](auto all_steps) {
 #pragma unroll
           for (int k = 0; k < S; ++k) {
-            if (decltype(all)::value || k < n) {
+            if (decltype(all_steps)::value || k < n) {
               h = RESET && (cuts >> k & 1) ? u[k] : vfma(a[k], h, u[k]);
               *reinterpret_cast<Raw*>(py) = Io::close(h);
               py += p.D;
             }
           }
         };
-        if (n >= S) write(std::true_type{});
-        else write(std::false_type{});
+        if (n >= S) write(Yes{});
+        else write(No{});
       }
     }
   }
