@@ -30,7 +30,9 @@ __device__ __forceinline__ Gates gates(float x, float gate, float in_gate, float
     float oa;
     decay_pair(r.g * A, r.a, oa);
     gate_pair(in_gate, r.iota, r.oi);
-    input_scale(oa, r.beta, r.inv);
+    const float m2 = one_minus_square(oa);
+    r.inv = rsqrt_approx(m2);
+    r.beta = m2 * r.inv;
     r.u = r.beta * r.iota * x;
   }
   return r;
@@ -130,6 +132,7 @@ ssm_status_t validate(const ssm_gated_problem_t* p) {
     if (ld > INT64_MAX / 8 / rows) return SSM_ERR_INVALID_ARG;    // (byte offsets stay within 63 bits)
   }
   if (!decay(*p) && (p->ld_in_gate != 0 || p->ld_din_gate != 0)) return SSM_ERR_INVALID_ARG;
+  if (p->D > 1 << 28) return SSM_ERR_UNSUPPORTED;                // (a row's bytes fit 32 bits)
   // blocks of the grids, 32 channels of one batch entry at the least
   if ((int64_t)p->batch * (((int64_t)p->D + 31) / 32) > INT32_MAX / 16) return SSM_ERR_UNSUPPORTED;
   if (p->L > INT32_MAX - 65536) return SSM_ERR_UNSUPPORTED;     // (steps of a round past the end)

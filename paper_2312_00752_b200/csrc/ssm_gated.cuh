@@ -2,6 +2,8 @@
 // sums and products issue two-wide), and what its kernels share.
 #pragma once
 
+#include <cfloat>
+
 #include "ssm_common.cuh"
 #include "ssm_gated.h"
 
@@ -55,14 +57,6 @@ __device__ __forceinline__ float2 vmap(float2 a, float2 b, float2 c, Op&& op) { 
 template <class F>
 constexpr int kWidth = sizeof(F) / sizeof(float);
 
-// Gates of bf16 io come no lower than this in the decay form (sigma: 1e-19), see gate_two.
-constexpr float kGateFloor = -43.5f;
-__device__ __forceinline__ float floor_gate(float z) {   // (NaN stays)
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(kGateFloor));
-  return r;
-}
-
 // `F` of adjacent channels as they lie in memory
 template <typename IO, class F>
 struct Lane;
@@ -82,18 +76,12 @@ template <>
 struct Lane<__nv_bfloat16, float> {
   using Raw = unsigned short;
   static __device__ __forceinline__ float open(unsigned short r) { return __uint_as_float((uint32_t)r << 16); }
-  static __device__ __forceinline__ float open_gate(unsigned short r) { return floor_gate(open(r)); }
   static __device__ __forceinline__ unsigned short close(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 };
 template <>
 struct Lane<__nv_bfloat16, float2> {
   using Raw = uint32_t;
   static __device__ __forceinline__ float2 open(uint32_t r) { return make_float2(bf16lo(r), bf16hi(r)); }
-  static __device__ __forceinline__ float2 open_gate(uint32_t r) {   // max(gate, kGateFloor), both at once (NaN stays)
-    uint32_t v;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(r), "r"(0xc22ec22eu));
-    return open(v);
-  }
   static __device__ __forceinline__ uint32_t close(float2 v) {
     const __nv_bfloat162 r = __floats2bfloat162_rn(v.x, v.y);
     return *reinterpret_cast<const uint32_t*>(&r);
@@ -147,44 +135,30 @@ __device__ __forceinline__ void decay_pair_small(F w, F& a, F& oa) {
   a = vfma(oa, vset<F>(-1.f), vset<F>(1.f));
 }
 
-// sigma of two gates with one reciprocal, 1 / ((1 + e1) (1 + e2)): the special-function unit, four lanes a cycle, is what limits
-// bf16 io next to the memory.  The gates come no lower than kGateFloor, so that the product stays in range.
+// 1 - a^2 = oa (2 - oa).  The least normal number keeps its reciprocal root finite where a = 1: that meets rho or A, which is 0
+// there, and the root itself is 1e-19 instead of 0.
 template <class F>
-__device__ __forceinline__ void gate_two(F z1, F z2, F& g1, F& g2) {
-  const F d1 = vadd(vmap(vmul(z1, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f));
-  const F d2 = vadd(vmap(vmul(z2, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f));
-  const F r = vmap(vmul(d1, d2), [](float v) { return rcp_approx(v); });
-  g1 = vmul(r, d2);
-  g2 = vmul(r, d1);
-}
-// sqrt(1 - a^2) = sqrt(oa (2 - oa)) and its reciprocal, which is 0 where a = 1
-template <class F>
-__device__ __forceinline__ void input_scale(F oa, F& beta, F& inv) {
-  const F m2 = vmul(oa, vfma(oa, vset<F>(-1.f), vset<F>(2.f)));
-  inv = vmap(m2, [](float v) { return rsqrt_approx(fmaxf(v, 1e-37f)); });   // (1 / beta meets rho, which is 0 there, or so near)
-  beta = vmul(m2, inv);
+__device__ __forceinline__ F one_minus_square(F oa) {
+  return vfma(oa, vfma(oa, vset<F>(-1.f), vset<F>(2.f)), vset<F>(FLT_MIN));
 }
 
-// One step of the forward recurrence: retention a and input u.  PAIRED: the gates share a reciprocal; SMALL: -1 <= A <= 0, and A
-// comes negated.
-template <bool DECAY, bool PAIRED, bool SMALL, class F>
+// One step of the forward recurrence: retention a and input u.  SMALL: -1 <= A <= 0, and A comes negated.
+// The special-function unit, four lanes a cycle, limits bf16 io next to the memory, so beta and the input gate come from
+// one operation: with f = 1 + exp(-in_gate), m2 rsqrt(m2 f^2) = sqrt(m2) / f = beta iota (f^2 may be infinite: then it is 0).
+template <bool DECAY, bool SMALL, class F>
 __device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F& u) {
-  F g, og;
+  F g;
   if constexpr (!DECAY) {
     gate_pair(gate, g, a);
     u = vmul(g, x);
   } else {
-    F oa, iota, oi, beta, inv;
-    if constexpr (PAIRED) {
-      gate_two(gate, in_gate, g, iota);
-    } else {
-      gate_pair(gate, g, og);
-      gate_pair(in_gate, iota, oi);
-    }
+    F oa;
+    g = vmap(vadd(vmap(vmul(gate, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f)), [](float v) { return rcp_approx(v); });
+    const F f = vadd(vmap(vmul(in_gate, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f));
     if constexpr (SMALL) decay_pair_small(vmul(g, A), a, oa);
     else decay_pair(vmul(g, A), a, oa);
-    input_scale(oa, beta, inv);
-    u = vmul(vmul(beta, iota), x);
+    const F m2 = one_minus_square(oa);
+    u = vmul(vmul(m2, vmap(vmul(vmul(m2, f), f), [](float v) { return rsqrt_approx(v); })), x);
   }
 }
 #endif

@@ -94,7 +94,7 @@ __device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase
   for (int i = 0; i < kWaitLimit; ++i) {
     unsigned done;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
         : "r"(shared_address(barrier)), "r"(phase)
         : "memory");
@@ -103,9 +103,9 @@ __device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase
   return false;
 }
 
-// The inputs of a warp's steps on their way from global memory: kAhead tiles ahead, through buffers of the warp's own in shared
-// memory that asynchronous copies of COPY bytes fill (16: a row of the warp's channels is cut among its lanes; 4: every
-// lane copies what it will read itself), or, for COPY = 0, elements too small for such copies, one tile ahead through registers.
+// The inputs of a warp's steps on their way from global memory, a tile ahead: two buffers of half the steps each, of the warp's own
+// in shared memory, that asynchronous copies of COPY bytes fill again as soon as they are read (16: a row of the warp's channels is cut
+// among its lanes; 4: every lane copies what it will read itself); or, for COPY = 0, elements too small for such copies, registers.
 __device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
 }
@@ -113,14 +113,13 @@ __device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid
 template <typename IO, class F, bool DECAY, int COPY>
 struct Feed {
   using Raw = typename Lane<IO, F>::Raw;
-  static constexpr int kAhead = COPY > 0 ? 2 : 1;
   static constexpr int kTensors = DECAY ? 3 : 2;
-  static constexpr int kRow = 32 * (int)sizeof(Raw);                          // bytes of a row of the warp's channels
-  static constexpr int kBytes = COPY > 0 ? kAhead * kTensors * S * kRow : 0;  // of shared memory for a warp
-  static constexpr int kLanes = COPY == 16 ? kRow / 16 : 32;                  // lanes that copy a row
-  static constexpr int kRows = 32 / kLanes;                                   // rows that the warp copies at once
+  static constexpr int kRow = 32 * (int)sizeof(Raw);                    // bytes of a row of the warp's channels
+  static constexpr int kBytes = COPY > 0 ? kTensors * S * kRow : 0;     // of shared memory for a warp
+  static constexpr int kLanes = COPY == 16 ? kRow / 16 : 32;            // lanes that copy a row
+  static constexpr int kRows = 32 / kLanes;                             // rows that the warp copies at once
 
-  const char* next[kTensors];   // this lane's first element (or chunk) in its first row of the next tile to fetch
+  const char* next[kTensors];   // this lane's first element (or chunk) in its first row of the next half to fetch
   int64_t ld[kTensors];         // bytes
   char* buf;
   int lane;
@@ -140,43 +139,44 @@ struct Feed {
       next[i] = static_cast<const char*>(ptr[i]) + (row + lane / kLanes) * ld[i] + (live ? at : 0) * (int)sizeof(IO);
     }
   }
-  // fetches the next tile's rows, n of them (S at most), and moves on by `step` rows
-  template <bool ALL>
-  __device__ __forceinline__ void rows(int n, int stage) {
+  template <int HALF, bool ALL>
+  __device__ __forceinline__ void rows(int n) {
 #pragma unroll
     for (int i = 0; i < kTensors; ++i) {
       const char* src = next[i];
-#pragma unroll(COPY == 4 ? 4 : S / kRows)
-      for (int k = 0; k < S / kRows; ++k, src += kRows * ld[i]) {
+#pragma unroll(COPY == 4 ? 4 : S / 2 / kRows)
+      for (int k = 0; k < S / 2 / kRows; ++k, src += kRows * ld[i]) {
         const int row = k * kRows + lane / kLanes;
         if constexpr (COPY > 0) {
-          char* dst = buf + ((stage * kTensors + i) * S + row) * kRow + lane % kLanes * COPY;
+          char* dst = buf + ((i * 2 + HALF) * (S / 2) + row) * kRow + lane % kLanes * COPY;
           const bool ok = live && (ALL || row < n);
-          const char* from = ALL || row < n ? src : next[i];     // (n > 0, but this lane's first row may be past it)
+          const char* from = ALL || row < n ? src : next[i];     // (not read where the row is not one)
           if constexpr (COPY == 16) cp_async16(dst, from, ok);
           else cp_async4(dst, from, ok);
         } else if (ALL || row < n) {
-          raw[i][k] = *reinterpret_cast<const Raw*>(src);
+          raw[i][HALF * (S / 2) + k] = *reinterpret_cast<const Raw*>(src);
         }
       }
     }
   }
-  __device__ __forceinline__ void issue(int n, int stage, int step) {
-    if (n >= S) rows<true>(n, stage);
-    else if (n > 0) rows<false>(n, stage);
+  // fetches the next half of a tile, n rows (S / 2 at most), and moves on by `step` rows
+  template <int HALF>
+  __device__ __forceinline__ void issue(int n, int step) {
+    if (n >= S / 2) rows<HALF, true>(n);
+    else if (n > 0) rows<HALF, false>(n);
     if constexpr (COPY > 0) cp_async_commit();
 #pragma unroll
     for (int i = 0; i < kTensors; ++i) next[i] += step * ld[i];
   }
-  __device__ __forceinline__ void arrive() {   // the oldest tile under way is there
+  __device__ __forceinline__ void arrive() {   // the older half under way is there
     if constexpr (COPY > 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
     if constexpr (COPY == 16) __syncwarp();
   }
   __device__ __forceinline__ void release() {  // every lane has read its values
     if constexpr (COPY == 16) __syncwarp();
   }
-  __device__ __forceinline__ Raw get(int i, int k, int stage) const {
-    if constexpr (COPY > 0) return *reinterpret_cast<const Raw*>(buf + ((stage * kTensors + i) * S + k) * kRow + lane * (int)sizeof(Raw));
+  __device__ __forceinline__ Raw get(int i, int k) const {   // step k of the tile
+    if constexpr (COPY > 0) return *reinterpret_cast<const Raw*>(buf + (i * S + k) * kRow + lane * (int)sizeof(Raw));
     else return raw[i][k];
   }
 };
@@ -186,8 +186,7 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
   using Io = Lane<IO, F>;
   using Raw = typename Io::Raw;
   using In = Feed<IO, F, DECAY, COPY>;
-  constexpr int V = kWidth<F>, kAhead = In::kAhead;
-  constexpr bool PAIRED = sizeof(IO) == 2;
+  constexpr int V = kWidth<F>;
   extern __shared__ __align__(16) char s_feed[];
   __shared__ Affine<F> s_warp[2][W][32];
   __shared__ Affine<F> s_block[2][kMaxCluster][32];
@@ -213,8 +212,8 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
   in.init(p, row0 + t0, d0, s_feed + w * In::kBytes, lane);
   dependency_wait();
 
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) in.issue(p.L - t0 - i * step, i, step);
+  in.template issue<0>(p.L - t0, S / 2);
+  in.template issue<1>(p.L - t0 - S / 2, step - S / 2);
   // bytes of the mask: those of the tile after the next are loaded where those of this one are looked at
   const uint8_t* __restrict__ pr = RESET ? p.reset + row0 : nullptr;
   auto mask_at = [&](int t) -> unsigned { return RESET && lane < S && t + lane < p.L ? pr[t + lane] : 0u; };
@@ -239,17 +238,14 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
     const unsigned cuts = RESET ? __ballot_sync(~0u, mask0 != 0) : 0u;   // bit k: step k of this warp resets
     mask0 = mask1;
     mask1 = mask_at(t0 + 2 * step);
-    in.arrive();
-    auto read = [&](auto all_steps, auto small_A) {
+    auto read = [&](auto first, auto all_steps, auto small_A) {   // steps first .. first + S / 2
       constexpr bool SMALL = decltype(small_A)::value;
       const F At = SMALL ? vmul(A, vset<F>(-1.f)) : A;
 #pragma unroll
-      for (int k = 0; k < S; ++k) {
+      for (int k = decltype(first)::value; k < decltype(first)::value + S / 2; ++k) {
         if (decltype(all_steps)::value || k < n) {
-          const F x = Io::open(in.get(0, k, half));
-          if constexpr (!DECAY) step_inputs<false, false, false>(x, Io::open(in.get(1, k, half)), x, x, a[k], u[k]);
-          else if constexpr (PAIRED) step_inputs<true, true, SMALL>(x, Io::open_gate(in.get(1, k, half)), Io::open_gate(in.get(2, k, half)), At, a[k], u[k]);
-          else step_inputs<true, false, SMALL>(x, Io::open(in.get(1, k, half)), Io::open(in.get(2, k, half)), At, a[k], u[k]);
+          const F x = Io::open(in.get(0, k));
+          step_inputs<DECAY, SMALL>(x, Io::open(in.get(1, k)), DECAY ? Io::open(in.get(DECAY ? 2 : 0, k)) : x, At, a[k], u[k]);
           if (RESET && (cuts >> k & 1)) {
             mine = {vset<F>(0.f), u[k]};
           } else {
@@ -261,15 +257,22 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
     };
     using Yes = std::true_type;
     using No = std::false_type;
-    if (n >= S) {
-      if (DECAY && small) read(Yes{}, Yes{});
-      else read(Yes{}, No{});
-    } else if (n > 0) {
-      if (DECAY && small) read(No{}, Yes{});
-      else read(No{}, No{});
-    }
-    in.release();
-    in.issue(n - kAhead * step, kAhead == 2 ? half : 0, step);
+    auto read_half = [&](auto first) {
+      if (n >= S) {
+        if (DECAY && small) read(first, Yes{}, Yes{});
+        else read(first, Yes{}, No{});
+      } else if (n > 0) {
+        if (DECAY && small) read(first, No{}, Yes{});
+        else read(first, No{}, No{});
+      }
+      in.release();
+    };
+    in.arrive();
+    read_half(std::integral_constant<int, 0>{});
+    in.template issue<0>(n - step, S / 2);
+    in.arrive();
+    read_half(std::integral_constant<int, S / 2>{});
+    in.template issue<1>(n - step - S / 2, step - S / 2);
     if (!RESET || cuts == 0) mine.P = vmap(mine.P, [](float v) { return fmaxf(v, FLT_MIN); });
 
     s_warp[half][w][lane] = mine;
@@ -305,14 +308,14 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
     if (live && n > 0) {
       if (p.states != nullptr) *reinterpret_cast<F*>(p.states + ((int64_t)b * p.nck + t0 / S) * p.D + d) = h;
       if (p.y != nullptr) {
-        IO* __restrict__ py = static_cast<IO*>(p.y) + (row0 + t0) * p.D + d;
+        char* __restrict__ py = reinterpret_cast<char*>(static_cast<IO*>(p.y) + (row0 + t0) * p.D + d);
+        const unsigned ld = (unsigned)p.D * (unsigned)sizeof(IO);
         auto write = [&](auto all_steps) {
 #pragma unroll
           for (int k = 0; k < S; ++k) {
             if (decltype(all_steps)::value || k < n) {
               h = RESET && (cuts >> k & 1) ? u[k] : vfma(a[k], h, u[k]);
-              *reinterpret_cast<Raw*>(py) = Io::close(h);
-              py += p.D;
+              *reinterpret_cast<Raw*>(py + (uint64_t)ld * k) = Io::close(h);
             }
           }
         };
