@@ -16,76 +16,6 @@ __device__ __forceinline__ void put(void* base, int64_t row, int64_t ld, int d, 
   static_cast<IO*>(base)[row * ld + d] = float_to_io<IO>(v);
 }
 
-// One step, with what its gradients need: the gate g (or rho) and 1 - g, the input gate and 1 - iota, beta = sqrt(1 - a^2).
-struct Gates {
-  float a, u, g, og, iota, oi, beta, inv;
-};
-template <bool DECAY>
-__device__ __forceinline__ Gates gates(float x, float gate, float in_gate, float A) {
-  Gates r{};
-  gate_pair(gate, r.g, r.og);
-  r.a = r.og;
-  r.u = r.g * x;
-  if constexpr (DECAY) {
-    float oa;
-    decay_pair(r.g * A, r.a, oa);
-    gate_pair(in_gate, r.iota, r.oi);
-    const float m2 = one_minus_square(oa);
-    r.inv = rsqrt_approx(m2);
-    r.beta = m2 * r.inv;
-    r.u = r.beta * r.iota * x;
-  }
-  return r;
-}
-
-template <typename IO, bool DECAY>
-__global__ void __launch_bounds__(kThreads) ssm_gated_bwd_kernel(const GatedParams p) {
-  dependency_wait();
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= (int64_t)p.batch * p.D) return;
-  const int b = (int)(i / p.D), d = (int)(i % p.D);
-  const float A = DECAY ? p.A[d] : 0.f;
-  float carry = p.dh_last != nullptr ? p.dh_last[i] : 0.f;   // a[t+1] mu[t+1]
-  float dA = 0.f;
-  for (int k0 = p.nck - 1; k0 >= 0; --k0) {
-    const int t0 = k0 * kGatedSteps, n = min(kGatedSteps, p.L - t0);
-    float before[kGatedSteps];     // the state that each step starts from
-    float h = p.states[((int64_t)b * p.nck + k0) * p.D + d];
-#pragma unroll
-    for (int j = 0; j < kGatedSteps; ++j) {
-      if (j < n) {
-        const int64_t row = (int64_t)b * p.L + t0 + j;
-        const Gates k = gates<DECAY>(at<IO>(p.x, row, p.ld_x, d), at<IO>(p.gate, row, p.ld_gate, d),
-                                     DECAY ? at<IO>(p.in_gate, row, p.ld_in, d) : 0.f, A);
-        before[j] = p.reset != nullptr && p.reset[row] ? 0.f : h;
-        h = p.reset != nullptr && p.reset[row] ? k.u : fmaf(k.a, h, k.u);
-      }
-    }
-#pragma unroll
-    for (int j = kGatedSteps - 1; j >= 0; --j) {
-      if (j < n) {
-        const int64_t row = (int64_t)b * p.L + t0 + j;
-        const float x = at<IO>(p.x, row, p.ld_x, d);
-        const Gates k = gates<DECAY>(x, at<IO>(p.gate, row, p.ld_gate, d), DECAY ? at<IO>(p.in_gate, row, p.ld_in, d) : 0.f, A);
-        const float mu = at<IO>(p.dy, row, p.D, d) + carry;
-        if constexpr (DECAY) {
-          const float m = mu * k.a * fmaf(-k.a * k.iota, x * k.inv, before[j]);
-          put<IO>(p.dx, row, p.ld_dx, d, mu * k.beta * k.iota);
-          put<IO>(p.din_gate, row, p.ld_din, d, mu * k.u * k.oi);
-          put<IO>(p.dgate, row, p.ld_dgate, d, m * A * k.g * k.og);
-          dA = fmaf(m, k.g, dA);
-        } else {
-          put<IO>(p.dx, row, p.ld_dx, d, mu * k.g);
-          put<IO>(p.dgate, row, p.ld_dgate, d, mu * (x - before[j]) * k.g * k.og);
-        }
-        carry = p.reset != nullptr && p.reset[row] ? 0.f : mu * k.a;
-      }
-    }
-  }
-  if (p.dh0 != nullptr) p.dh0[i] = carry;
-  if (DECAY) p.dA_part[i] = dA;
-}
-
 // dA[d]: the parts in ascending order
 __global__ void __launch_bounds__(kThreads) ssm_gated_reduce_kernel(const float* __restrict__ part, int parts, int D,
                                                                   float* __restrict__ dA) {
@@ -104,9 +34,10 @@ __global__ void __launch_bounds__(kThreads) ssm_gated_step_kernel(const GatedPar
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   if (i >= (int64_t)p.batch * p.D) return;
   const int b = (int)(i / p.D), d = (int)(i % p.D);
-  const Gates k = gates<DECAY>(at<IO>(p.x, b, p.ld_x, d), at<IO>(p.gate, b, p.ld_gate, d),
-                               DECAY ? at<IO>(p.in_gate, b, p.ld_in, d) : 0.f, DECAY ? p.A[d] : 0.f);
-  const float h = p.reset != nullptr && p.reset[b] ? k.u : fmaf(k.a, hbuf[i], k.u);
+  float a, u;
+  step_inputs<DECAY, false>(at<IO>(p.x, b, p.ld_x, d), at<IO>(p.gate, b, p.ld_gate, d), DECAY ? at<IO>(p.in_gate, b, p.ld_in, d) : 0.f,
+                            DECAY ? p.A[d] : 0.f, a, u);
+  const float h = p.reset != nullptr && p.reset[b] ? u : fmaf(a, hbuf[i], u);
   hbuf[i] = h;
   put<IO>(p.y, b, p.D, d, h);
 }
@@ -126,13 +57,12 @@ ssm_status_t validate(const ssm_gated_problem_t* p) {
   if (p->flags & ~(uint32_t)(SSM_GATED_FLAG_DECAY | SSM_GATED_FLAG_SAVE_STATES)) return SSM_ERR_INVALID_ARG;
   if (p->io_dtype != SSM_F32 && p->io_dtype != SSM_BF16) return SSM_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)p->batch * p->L;
-  if (p->D > INT64_MAX / 8 / rows) return SSM_ERR_UNSUPPORTED;
+  if (p->D > 1 << 28 || rows > INT64_MAX >> 32) return SSM_ERR_UNSUPPORTED;   // (byte offsets stay within 63 bits)
   for (int64_t ld : {p->ld_x, p->ld_gate, p->ld_in_gate, p->ld_dx, p->ld_dgate, p->ld_din_gate}) {
     if (ld != 0 && ld < p->D) return SSM_ERR_INVALID_ARG;
-    if (ld > INT64_MAX / 8 / rows) return SSM_ERR_INVALID_ARG;    // (byte offsets stay within 63 bits)
+    if (ld > 1 << 28) return SSM_ERR_UNSUPPORTED;                 // (a row's bytes fit 32 bits)
   }
   if (!decay(*p) && (p->ld_in_gate != 0 || p->ld_din_gate != 0)) return SSM_ERR_INVALID_ARG;
-  if (p->D > 1 << 28) return SSM_ERR_UNSUPPORTED;                // (a row's bytes fit 32 bits)
   // blocks of the grids, 32 channels of one batch entry at the least
   if ((int64_t)p->batch * (((int64_t)p->D + 31) / 32) > INT32_MAX / 16) return SSM_ERR_UNSUPPORTED;
   if (p->L > INT32_MAX - 65536) return SSM_ERR_UNSUPPORTED;     // (steps of a round past the end)
@@ -159,12 +89,9 @@ GatedParams params(const ssm_gated_problem_t& p) {
 size_t state_bytes(const ssm_gated_problem_t& p) {
   return (size_t)p.batch * ((p.L + kGatedSteps - 1) / kGatedSteps) * p.D * sizeof(float);
 }
+size_t part_bytes(const ssm_gated_problem_t& p) { return decay(p) ? (size_t)p.batch * kGatedCluster * p.D * sizeof(float) : 0; }
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-template <typename IO>
-cudaError_t launch_backward(const GatedParams& p, bool dec, cudaStream_t s) {
-  return dec ? launch_channels(ssm_gated_bwd_kernel<IO, true>, p, s, p) : launch_channels(ssm_gated_bwd_kernel<IO, false>, p, s, p);
-}
 template <typename IO>
 cudaError_t launch_step(const GatedParams& p, float* h, bool dec, cudaStream_t s) {
   return dec ? launch_channels(ssm_gated_step_kernel<IO, true>, p, s, p, h) : launch_channels(ssm_gated_step_kernel<IO, false>, p, s, p, h);
@@ -223,8 +150,7 @@ ssm_status_t ssm_gated_fwd(const ssm_gated_problem_t* p, const void* x, const vo
 
 size_t ssm_gated_bwd_workspace_bytes(const ssm_gated_problem_t* p) {
   if (validate(p) != SSM_OK) return 0;
-  const size_t parts = decay(*p) ? (size_t)p->batch * p->D * sizeof(float) : 0;
-  return round16(parts) + (p->flags & SSM_GATED_FLAG_SAVE_STATES ? 0 : state_bytes(*p));
+  return round16(part_bytes(*p)) + (p->flags & SSM_GATED_FLAG_SAVE_STATES ? 0 : state_bytes(*p));
 }
 
 ssm_status_t ssm_gated_bwd(const ssm_gated_problem_t* p, const void* x, const void* gate, const void* in_gate, const float* A,
@@ -254,9 +180,8 @@ ssm_status_t ssm_gated_bwd(const ssm_gated_problem_t* p, const void* x, const vo
   g.dA_part = static_cast<float*>(workspace);
   g.states = const_cast<float*>(saved_states);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool bf16 = p->io_dtype == SSM_BF16;
   if (!saved) {
-    g.states = reinterpret_cast<float*>(static_cast<char*>(workspace) + round16(dec ? (size_t)p->batch * p->D * sizeof(float) : 0));
+    g.states = reinterpret_cast<float*>(static_cast<char*>(workspace) + round16(part_bytes(*p)));
     if (launch_gated_fwd(g, p->io_dtype, dec, unit(*p, g), s) != cudaSuccess) return SSM_ERR_CUDA;
   }
   g.dy = dy;
@@ -265,10 +190,10 @@ ssm_status_t ssm_gated_bwd(const ssm_gated_problem_t* p, const void* x, const vo
   g.dgate = dgate;
   g.din_gate = din_gate;
   g.dh0 = dh0;
-  const cudaError_t e = bf16 ? launch_backward<__nv_bfloat16>(g, dec, s) : launch_backward<float>(g, dec, s);
-  if (e != cudaSuccess) return SSM_ERR_CUDA;
+  int parts = 0;
+  if (launch_gated_bwd(g, p->io_dtype, dec, unit(*p, g), &parts, s) != cudaSuccess) return SSM_ERR_CUDA;
   if (!dec) return SSM_OK;
-  return status(launch_dependent(ssm_gated_reduce_kernel, (p->D + kThreads - 1) / kThreads, kThreads, 0, 1, s, g.dA_part, p->batch,
+  return status(launch_dependent(ssm_gated_reduce_kernel, (p->D + kThreads - 1) / kThreads, kThreads, 0, 1, s, g.dA_part, parts,
                                  p->D, dA));
 }
 

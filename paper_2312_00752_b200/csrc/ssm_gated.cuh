@@ -9,6 +9,9 @@
 
 namespace ssm {
 
+constexpr int kGatedSteps = 8;     // steps between two saved states
+constexpr int kGatedCluster = 8;   // blocks of a cluster at most
+
 struct GatedParams {
   const void* x;
   const void* gate;
@@ -161,13 +164,98 @@ __device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F
     u = vmul(vmul(m2, vmap(vmul(vmul(m2, f), f), [](float v) { return rsqrt_approx(v); })), x);
   }
 }
+// ---------------------------------------------------------------------------------------------------- runs of steps
+// What a run of steps does to the state that enters it: h -> P h + S.
+template <class F>
+struct alignas(2 * sizeof(F)) Affine {
+  F P, S;
+};
+
+// the state behind a run of steps; RESET: P = 0 lets nothing pass
+template <bool RESET, class F>
+__device__ __forceinline__ F apply(const Affine<F>& k, F h) {
+  const F r = vfma(k.P, h, k.S);
+  if constexpr (!RESET) return r;
+  return vmap(k.P, k.S, r, [](float P, float s, float v) { return P == 0.f ? s : v; });
+}
+template <bool RESET, class F>
+__device__ __forceinline__ Affine<F> then(const Affine<F>& first, const Affine<F>& second) {
+  Affine<F> r;
+  r.S = apply<RESET>(second, first.S);
+  r.P = vmul(second.P, first.P);
+  if constexpr (RESET)
+    r.P = vmap(r.P, first.P, second.P, [](float v, float a, float b) { return a == 0.f || b == 0.f ? 0.f : fmaxf(v, FLT_MIN); });
+  else
+    r.P = vmap(r.P, [](float v) { return fmaxf(v, FLT_MIN); });
+  return r;
+}
+
+// --------------------------------------------------------------------------------------- between the blocks of a cluster
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ unsigned cluster_size() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned shared_address(const void* q) { return (unsigned)__cvta_generic_to_shared(q); }
+__device__ __forceinline__ unsigned remote_address(const void* local, unsigned rank) {   // the same place in block `rank`
+  unsigned r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(shared_address(local)), "r"(rank));
+  return r;
+}
+// A store into another block's shared memory that counts its bytes at a barrier there: the reader waits for the bytes, and the
+// writer for nothing.  (A barrier of the whole cluster with its release waits for every store of y under way and every copy: 1.5
+// of the 9.6 cycles between two instructions of a warp.)
+__device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine<float>& v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.P), "f"(v.S), "r"(barrier) : "memory");
+}
+__device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine<float2>& v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "f"(v.P.x), "f"(v.P.y),
+               "f"(v.S.x), "f"(v.S.y), "r"(barrier)
+               : "memory");
+}
+__device__ __forceinline__ void barrier_init(const void* barrier) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(barrier)) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(const void* barrier, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
+}
+// Waits for the bytes of a phase.  The blocks of a cluster run at the same time and send before they wait, so that every wait
+// ends; the limit (seconds) keeps a fault elsewhere from holding the GPU.  False: it was reached.
+constexpr int kWaitLimit = 1 << 20;
+__device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase) {
+  for (int i = 0; i < kWaitLimit; ++i) {
+    unsigned done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(shared_address(barrier)), "r"(phase)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+
+__device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+
 #endif
 
 // ------------------------------------------------------------------------------------------------------------ launches
-// Steps of one warp in a tile, and between two saved states.
-constexpr int kGatedSteps = 16;
 
 // unit: bytes (16, 4 or, for bf16, 2) whose multiples the io pointers and the distances of rows are, D too
 cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, int unit, cudaStream_t s);
+// parts: how many rows of dA_part were written
+cudaError_t launch_gated_bwd(const GatedParams& p, int io_dtype, bool decay, int unit, int* parts, cudaStream_t s);
+// Blocks that share the tiles of a group of channels: `rounds(c)` of a tile each, `tiles` groups, `resident` blocks at once.
+int choose_gated_cluster(long long tiles, long long steps, int tile_steps, long long resident);
 
 }  // namespace ssm

@@ -11,7 +11,6 @@
 // P may underflow although no retention is zero, and zero times an infinite state would be NaN where the steps one by one
 // keep it infinite: it is held at the least normal number, 2^-126 of the state at most, far below its rounding.  A step that
 // resets makes P exactly zero, and zero stands for "nothing of the state passes", infinite or not.
-#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -21,95 +20,13 @@ namespace ssm {
 
 namespace {
 
-constexpr int S = kGatedSteps;
+constexpr int S = 16;                // steps of a warp in a tile
 constexpr int W = 4;                 // warps of a block
 constexpr int kTile = S * W;         // steps of a tile
-constexpr int kMaxCluster = 8;
-
-template <class F>
-struct alignas(2 * sizeof(F)) Affine {
-  F P, S;
-};
-
-// the state behind a run of steps; RESET: P = 0 lets nothing pass
-template <bool RESET, class F>
-__device__ __forceinline__ F apply(const Affine<F>& k, F h) {
-  const F r = vfma(k.P, h, k.S);
-  if constexpr (!RESET) return r;
-  return vmap(k.P, k.S, r, [](float P, float s, float v) { return P == 0.f ? s : v; });
-}
-template <bool RESET, class F>
-__device__ __forceinline__ Affine<F> then(const Affine<F>& first, const Affine<F>& second) {
-  Affine<F> r;
-  r.S = apply<RESET>(second, first.S);
-  r.P = vmul(second.P, first.P);
-  if constexpr (RESET)
-    r.P = vmap(r.P, first.P, second.P, [](float v, float a, float b) { return a == 0.f || b == 0.f ? 0.f : fmaxf(v, FLT_MIN); });
-  else
-    r.P = vmap(r.P, [](float v) { return fmaxf(v, FLT_MIN); });
-  return r;
-}
-
-// --------------------------------------------------------------------------------------- between the blocks of a cluster
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ unsigned cluster_size() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ unsigned shared_address(const void* q) { return (unsigned)__cvta_generic_to_shared(q); }
-__device__ __forceinline__ unsigned remote_address(const void* local, unsigned rank) {   // the same place in block `rank`
-  unsigned r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(shared_address(local)), "r"(rank));
-  return r;
-}
-// A store into another block's shared memory that counts its bytes at a barrier there: the reader waits for the bytes, and the
-// writer for nothing.  (A barrier of the whole cluster with its release waits for every store of y under way and every copy: 1.5
-// of the 9.6 cycles between two instructions of a warp.)
-__device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine<float>& v) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.P), "f"(v.S), "r"(barrier) : "memory");
-}
-__device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine<float2>& v) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "f"(v.P.x), "f"(v.P.y),
-               "f"(v.S.x), "f"(v.S.y), "r"(barrier)
-               : "memory");
-}
-__device__ __forceinline__ void barrier_init(const void* barrier) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(barrier)) : "memory");
-}
-__device__ __forceinline__ void barrier_expect(const void* barrier, unsigned bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
-}
-// Waits for the bytes of a phase.  The blocks of a cluster run at the same time and send before they wait, so that every wait
-// ends; the limit (seconds) keeps a fault elsewhere from holding the GPU.  False: it was reached.
-constexpr int kWaitLimit = 1 << 20;
-__device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase) {
-  for (int i = 0; i < kWaitLimit; ++i) {
-    unsigned done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(shared_address(barrier)), "r"(phase)
-        : "memory");
-    if (done) return true;
-  }
-  return false;
-}
 
 // The inputs of a warp's steps on their way from global memory, a tile ahead: two buffers of half the steps each, of the warp's own
 // in shared memory, that asynchronous copies of COPY bytes fill again as soon as they are read (16: a row of the warp's channels is cut
 // among its lanes; 4: every lane copies what it will read itself); or, for COPY = 0, elements too small for such copies, registers.
-__device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
-}
-
 template <typename IO, class F, bool DECAY, int COPY>
 struct Feed {
   using Raw = typename Lane<IO, F>::Raw;
@@ -189,7 +106,7 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
   constexpr int V = kWidth<F>;
   extern __shared__ __align__(16) char s_feed[];
   __shared__ Affine<F> s_warp[2][W][32];
-  __shared__ Affine<F> s_block[2][kMaxCluster][32];
+  __shared__ Affine<F> s_block[2][kGatedCluster][32];
   __shared__ uint64_t s_there[2];                    // one barrier for each half of s_block
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int C = (int)cluster_size(), rank = (int)cluster_rank();
@@ -306,16 +223,17 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
     }
 
     if (live && n > 0) {
-      if (p.states != nullptr) *reinterpret_cast<F*>(p.states + ((int64_t)b * p.nck + t0 / S) * p.D + d) = h;
-      if (p.y != nullptr) {
+      float* __restrict__ keep = p.states != nullptr ? p.states + ((int64_t)b * p.nck + t0 / kGatedSteps) * p.D + d : nullptr;
+      if (keep != nullptr || p.y != nullptr) {
         char* __restrict__ py = reinterpret_cast<char*>(static_cast<IO*>(p.y) + (row0 + t0) * p.D + d);
         const unsigned ld = (unsigned)p.D * (unsigned)sizeof(IO);
         auto write = [&](auto all_steps) {
 #pragma unroll
           for (int k = 0; k < S; ++k) {
             if (decltype(all_steps)::value || k < n) {
+              if (k % kGatedSteps == 0 && keep != nullptr) *reinterpret_cast<F*>(keep + (int64_t)(k / kGatedSteps) * p.D) = h;
               h = RESET && (cuts >> k & 1) ? u[k] : vfma(a[k], h, u[k]);
-              *reinterpret_cast<Raw*>(py + (uint64_t)ld * k) = Io::close(h);
+              if (p.y != nullptr) *reinterpret_cast<Raw*>(py + (uint64_t)ld * k) = Io::close(h);
             }
           }
         };
@@ -327,21 +245,6 @@ __global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedPar
   if (p.h_last != nullptr && live && w == 0 && rank == 0) *reinterpret_cast<F*>(p.h_last + (int64_t)b * p.D + d) = carry;
 }
 
-// Blocks of a cluster.  Blocks run in ceil(blocks / resident) turns of ceil(L / (cluster kTile)) rounds each.
-int choose_cluster(long long tiles, int L, long long resident) {
-  int best = 1;
-  long long best_cost = -1;
-  for (int c = 1; c <= kMaxCluster; c *= 2) {
-    const long long rounds = (L + (long long)kTile * c - 1) / ((long long)kTile * c);
-    const long long cost = (tiles * c + resident - 1) / resident * (rounds * (c > 1 ? 10 : 9) + 10);
-    if (best_cost < 0 || cost < best_cost) {
-      best_cost = cost;
-      best = c;
-    }
-  }
-  return best;
-}
-
 template <typename IO, class F, bool DECAY, bool RESET, int COPY>
 cudaError_t launch(GatedParams p, cudaStream_t s) {
   const auto kernel = ssm_gated_fwd_kernel<IO, F, DECAY, RESET, COPY>;
@@ -351,7 +254,7 @@ cudaError_t launch(GatedParams p, cudaStream_t s) {
   const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), 32 * W, smem, &lim);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.tiles * p.batch;
-  const int c = choose_cluster(tiles, p.L, (long long)lim.sms * lim.per_sm);
+  const int c = choose_gated_cluster(tiles, p.L, kTile, (long long)lim.sms * lim.per_sm);
   return launch_dependent(kernel, (unsigned)(tiles * c), 32 * W, smem, c, s, p);
 }
 
@@ -362,6 +265,22 @@ cudaError_t launch_form(const GatedParams& p, bool decay, cudaStream_t s) {
 }
 
 }  // namespace
+
+// Blocks run in ceil(blocks / resident) turns of so many rounds each, a round among several blocks costs a tenth more, and a block
+// takes a round's time to get going.
+int choose_gated_cluster(long long tiles, long long steps, int tile_steps, long long resident) {
+  int best = 1;
+  long long best_cost = -1;
+  for (int c = 1; c <= kGatedCluster; c *= 2) {
+    const long long rounds = (steps + (long long)tile_steps * c - 1) / ((long long)tile_steps * c);
+    const long long cost = (tiles * c + resident - 1) / resident * (rounds * (c > 1 ? 10 : 9) + 10);
+    if (best_cost < 0 || cost < best_cost) {
+      best_cost = cost;
+      best = c;
+    }
+  }
+  return best;
+}
 
 // Pairs of bf16 channels per lane (a row of a warp is a 128-byte line either way); float32 io has twice the bytes for the same
 // arithmetic and does without packed instructions.

