@@ -113,7 +113,7 @@ __device__ __forceinline__ F rest(F z, F g) {
 }
 
 template <typename IO, class F, bool DECAY, bool RESET, int COPY>
-__global__ void __launch_bounds__(32 * W, 4) ssm_gated_bwd_kernel(const GatedParams p) {
+__global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(const GatedParams p) {
   using Io = Lane<IO, F>;
   using Raw = typename Io::Raw;
   using In = Feed<IO, F, DECAY, COPY>;
