@@ -6,6 +6,7 @@
 
 #include "ssm_common.cuh"
 #include "ssm_gated.h"
+#include "ssm_pair.cuh"
 
 namespace ssm {
 
@@ -35,31 +36,6 @@ struct GatedParams {
 };
 
 #ifdef __CUDACC__
-// ------------------------------------------------------------------------------------------- one channel or two
-__device__ __forceinline__ float vmul(float a, float b) { return a * b; }
-__device__ __forceinline__ float2 vmul(float2 a, float2 b) { return f2mul(a, b); }
-__device__ __forceinline__ float vadd(float a, float b) { return a + b; }
-__device__ __forceinline__ float2 vadd(float2 a, float2 b) { return __fadd2_rn(a, b); }
-__device__ __forceinline__ float vfma(float a, float b, float c) { return fmaf(a, b, c); }
-__device__ __forceinline__ float2 vfma(float2 a, float2 b, float2 c) { return f2fma(a, b, c); }
-template <class F>
-__device__ __forceinline__ F vset(float v);
-template <>
-__device__ __forceinline__ float vset<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float2 vset<float2>(float v) { return make_float2(v, v); }
-template <class Op>
-__device__ __forceinline__ float vmap(float a, Op&& op) { return op(a); }
-template <class Op>
-__device__ __forceinline__ float2 vmap(float2 a, Op&& op) { return make_float2(op(a.x), op(a.y)); }
-template <class Op>
-__device__ __forceinline__ float vmap(float a, float b, float c, Op&& op) { return op(a, b, c); }
-template <class Op>
-__device__ __forceinline__ float2 vmap(float2 a, float2 b, float2 c, Op&& op) { return make_float2(op(a.x, b.x, c.x), op(a.y, b.y, c.y)); }
-
-template <class F>
-constexpr int kWidth = sizeof(F) / sizeof(float);
-
 // `F` of adjacent channels as they lie in memory
 template <typename IO, class F>
 struct Lane;

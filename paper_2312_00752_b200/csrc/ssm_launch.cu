@@ -34,7 +34,17 @@ cudaError_t kernel_limits(const void* kernel, int threads, size_t smem, KernelLi
   }
   KernelLimits k{};
   if ((e = cudaDeviceGetAttribute(&k.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-  if (smem > 0 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+  if (smem > 0) {
+    // All that the device allows, whatever this call asks for: a limit set to a smaller launch would refuse the larger ones
+    // that are in the table already.
+    cudaFuncAttributes at{};
+    int most = 0;
+    if ((e = cudaFuncGetAttributes(&at, kernel)) != cudaSuccess) return e;
+    if ((e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev)) != cudaSuccess) return e;
+    most -= (int)at.sharedSizeBytes;
+    if ((size_t)most < smem) return cudaErrorInvalidValue;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most)) != cudaSuccess) return e;
+  }
   if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k.per_sm, kernel, threads, smem)) != cudaSuccess) return e;
   if (k.per_sm < 1) return cudaErrorLaunchOutOfResources;
   known[key] = k;

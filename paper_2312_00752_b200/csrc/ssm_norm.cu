@@ -1,7 +1,11 @@
 // Norm of rows (layer norm, or without mean and bias) with the residual add in front of it, forward and backward.  See
 // include/ssm_norm.h for the definition.
+#include <cmath>
+#include <type_traits>
+
 #include "ssm_common.cuh"
 #include "ssm_norm.h"
+#include "ssm_pair.cuh"
 
 namespace ssm {
 
@@ -35,36 +39,70 @@ struct NormParams {
 // ------------------------------------------------------------------------------------------------------ rows in registers
 // A group of threads holds a row: NV vectors of VE adjacent elements a thread, vector k of thread j at (k group + j) VE, so that the
 // group's accesses are contiguous.  VE is 16 bytes of io, or one element where the rows do not allow such accesses.
+template <int VE>
+using Val = typename std::conditional<VE == 1, float, float2>::type;   // what arithmetic is done on
+template <int VE>
+constexpr int kVals = VE == 1 ? 1 : VE / 2;
+__device__ __forceinline__ float total(float v) { return v; }
+__device__ __forceinline__ float total(float2 v) { return v.x + v.y; }
+
 template <typename T, int VE>
-struct Row {   // VE elements of type T
-  T v[VE];
+struct Row {   // VE elements of type T as they lie in memory
+  using Word = typename std::conditional<VE == 1, T, uint4>::type;
+  static constexpr int kWords = VE == 1 ? 1 : VE * (int)sizeof(T) / 16;
+  Word w[kWords];
+  __device__ __forceinline__ void load(const void* base, int64_t at) {
+    const Word* q = reinterpret_cast<const Word*>(static_cast<const T*>(base) + at);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = q[i];
+  }
+  __device__ __forceinline__ void store(void* base, int64_t at) const {
+    Word* q = reinterpret_cast<Word*>(static_cast<T*>(base) + at);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) q[i] = w[i];
+  }
+  __device__ __forceinline__ void get(Val<VE> (&v)[kVals<VE>]) const {
+    if constexpr (VE == 1) {
+      v[0] = io_to_float<T>(w[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        const uint32_t r[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        if constexpr (sizeof(T) == 4) {
+          v[2 * i] = make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+          v[2 * i + 1] = make_float2(__uint_as_float(r[2]), __uint_as_float(r[3]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[4 * i + j] = make_float2(bf16lo(r[j]), bf16hi(r[j]));
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void set(const Val<VE> (&v)[kVals<VE>]) {   // rounded to T
+    if constexpr (VE == 1) {
+      w[0] = float_to_io<T>(v[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        uint32_t r[4];
+        if constexpr (sizeof(T) == 4) {
+          w[i] = make_uint4(__float_as_uint(v[2 * i].x), __float_as_uint(v[2 * i].y), __float_as_uint(v[2 * i + 1].x), __float_as_uint(v[2 * i + 1].y));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 c = __floats2bfloat162_rn(v[4 * i + j].x, v[4 * i + j].y);
+            r[j] = *reinterpret_cast<const uint32_t*>(&c);
+          }
+          w[i] = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+      }
+    }
+  }
 };
-template <typename T, int VE>
-__device__ __forceinline__ void load(Row<T, VE>& r, const void* base, int64_t at) {
-  const T* q = static_cast<const T*>(base) + at;
-  if constexpr (VE * sizeof(T) % 16 == 0) {
-#pragma unroll
-    for (int i = 0; i < (int)(VE * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(r.v)[i] = reinterpret_cast<const uint4*>(q)[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < VE; ++i) r.v[i] = q[i];
-  }
-}
-template <typename T, int VE>
-__device__ __forceinline__ void store(const Row<T, VE>& r, void* base, int64_t at) {
-  T* q = static_cast<T*>(base) + at;
-  if constexpr (VE * sizeof(T) % 16 == 0) {
-#pragma unroll
-    for (int i = 0; i < (int)(VE * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(q)[i] = reinterpret_cast<const uint4*>(r.v)[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < VE; ++i) q[i] = r.v[i];
-  }
-}
 
 constexpr int kMaxWarps = 32;
 // threads of a block, by vectors a thread: what the registers allow
-constexpr int fwd_threads(int VE, int NV) { return VE == 8 && NV == 4 ? 768 : 1024; }
+constexpr int fwd_threads(int VE, int NV) { return VE * NV > 48 ? 384 : VE * NV > 16 ? 512 : 1024; }
 constexpr int bwd_threads(int VE, int NV) {
   if (VE == 1) return 768;
   if (VE == 4) return NV == 1 ? 1024 : NV == 2 ? 640 : 384;
@@ -105,57 +143,101 @@ __global__ void __launch_bounds__(fwd_threads(VE, NV)) ssm_norm_rows_fwd_kernel(
   for (int k = 0; k < NV; ++k) {
     const int c = (k * group + j) * VE;
     if (c < p.D) {
-      load(x[k], p.x, at0 + c);
-      if (add) load(s[k], p.residual, at0 + c);
+      x[k].load(p.x, at0 + c);
+      if (add) s[k].load(p.residual, at0 + c);
     }
   }
-  float sum[1] = {0.f};
+  using F = Val<VE>;
+  constexpr int M = kVals<VE>;
+  F acc = vset<F>(0.f);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * group + j) * VE;
     if (c < p.D) {
+      F v[M], a[M];
+      x[k].get(v);
+      if (add) {
+        s[k].get(a);
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const float v = io_to_float<IO>(x[k].v[i]);
-        s[k].v[i] = float_to_io<RES>(add ? v + io_to_float<RES>(s[k].v[i]) : v);
-        sum[0] += io_to_float<RES>(s[k].v[i]);
+        for (int i = 0; i < M; ++i) v[i] = vadd(v[i], a[i]);
       }
-      if (p.residual_out != nullptr && live) store(s[k], p.residual_out, at0 + c);
+      s[k].set(v);
+      s[k].get(v);
+#pragma unroll
+      for (int i = 0; i < M; ++i) acc = vadd(acc, v[i]);
+      if (p.residual_out != nullptr && live) s[k].store(p.residual_out, at0 + c);
     }
   }
-  float m = 0.f;
+  const float over = 1.f / (float)p.D;
+  float m = 0.f, sum[1] = {total(acc)};
   if (!p.rms) {
     group_sum(sum, group, s_sum, 0);
-    m = sum[0] / (float)p.D;
+    m = sum[0] * over;
   }
-  sum[0] = 0.f;
+  const F off = vset<F>(-m);
+  acc = vset<F>(0.f);
 #pragma unroll
   for (int k = 0; k < NV; ++k)
-    if ((k * group + j) * VE < p.D)
+    if ((k * group + j) * VE < p.D) {
+      F v[M];
+      s[k].get(v);
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const float c = io_to_float<RES>(s[k].v[i]) - m;
-        sum[0] = fmaf(c, c, sum[0]);
+      for (int i = 0; i < M; ++i) {
+        const F c = vadd(v[i], off);
+        acc = vfma(c, c, acc);
       }
+    }
+  sum[0] = total(acc);
   group_sum(sum, group, s_sum, 1);
-  const float r = rsqrtf(sum[0] / (float)p.D + p.eps);
+  const float r = rsqrtf(fmaf(sum[0], over, p.eps));
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * group + j) * VE;
     if (c < p.D && live) {
       Row<float, VE> w, b;
       Row<IO, VE> y;
-      load(w, p.weight, c);
-      if (p.bias != nullptr) load(b, p.bias, c);
+      F v[M], wv[M], bv[M];
+      s[k].get(v);
+      w.load(p.weight, c);
+      w.get(wv);
+      if (p.bias != nullptr) {
+        b.load(p.bias, c);
+        b.get(bv);
+      }
 #pragma unroll
-      for (int i = 0; i < VE; ++i)
-        y.v[i] = float_to_io<IO>(fmaf((io_to_float<RES>(s[k].v[i]) - m) * r, w.v[i], p.bias != nullptr ? b.v[i] : 0.f));
-      store(y, p.y, at0 + c);
+      for (int i = 0; i < M; ++i) {
+        const F xh = vmul(vadd(v[i], off), vset<F>(r));
+        v[i] = p.bias != nullptr ? vfma(xh, wv[i], bv[i]) : vmul(xh, wv[i]);
+      }
+      y.set(v);
+      y.store(p.y, at0 + c);
     }
   }
   if (p.stats != nullptr && j == 0 && live) {
     p.stats[2 * here] = m;
     p.stats[2 * here + 1] = r;
+  }
+}
+
+// the sum of a block's groups' column sums v, in order; s_part: [groups][D] where there is more than one
+template <int VE, int NV>
+__device__ __forceinline__ void block_parts(float* __restrict__ out, const Val<VE> (&v)[NV][kVals<VE>], int D, int group, float* s_part) {
+  const int j = threadIdx.x % group, groups = blockDim.x / group;
+  if (groups > 1) __syncthreads();
+  float* to = groups > 1 ? s_part + threadIdx.x / group * D : out;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * group + j) * VE;
+#pragma unroll
+    for (int i = 0; i < kVals<VE>; ++i)
+      if (c < D) *reinterpret_cast<Val<VE>*>(to + c + i * kWidth<Val<VE>>) = v[k][i];
+  }
+  if (groups == 1) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < D; c += blockDim.x) {
+    float a = s_part[c];
+    for (int q = 1; q < groups; ++q) a += s_part[q * D + c];
+    out[c] = a;
   }
 }
 
@@ -172,13 +254,15 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
   const int64_t first = (int64_t)blockIdx.x * groups;    // (the block's groups run the same number of turns)
   int64_t here = first + threadIdx.x / group;
   dependency_wait();
-  float dw[NV][VE], db[BIAS ? NV : 1][BIAS ? VE : 1];
+  using F = Val<VE>;
+  constexpr int M = kVals<VE>;
+  F dw[NV][M], db[BIAS ? NV : 1][M];
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      dw[k][i] = 0.f;
-      if constexpr (BIAS) db[k][i] = 0.f;
+    for (int i = 0; i < M; ++i) {
+      dw[k][i] = vset<F>(0.f);
+      if constexpr (BIAS) db[k][i] = vset<F>(0.f);
     }
   Row<RES, VE> s[NV], sn[NV];
   Row<IO, VE> g[NV], gn[NV];
@@ -189,8 +273,8 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
         if (c < p.D) {
-          load(sn[k], p.s, row * p.D + c);
-          load(gn[k], p.dy, row * p.D + c);
+          sn[k].load(p.s, row * p.D + c);
+          gn[k].load(p.dy, row * p.D + c);
         }
       }
       mn = p.stats[2 * row];
@@ -214,29 +298,35 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) load(add[k], p.dresidual_out, here * p.D + c);
+        if (c < p.D) add[k].load(p.dresidual_out, here * p.D + c);
       }
     }
     fetch(here + apart);
-    float sum[2] = {0.f, 0.f};
+    const F off = vset<F>(-m);
+    F acc0 = vset<F>(0.f), acc1 = vset<F>(0.f);
     if (live) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
         if (c < p.D) {
           Row<float, VE> w;
-          load(w, p.weight, c);
+          F wv[M], sv[M], yv[M];
+          w.load(p.weight, c);
+          w.get(wv);
+          s[k].get(sv);
+          g[k].get(yv);
 #pragma unroll
-          for (int i = 0; i < VE; ++i) {
-            const float gy = io_to_float<IO>(g[k].v[i]), q = gy * w.v[i], xh = (io_to_float<RES>(s[k].v[i]) - m) * r;
-            sum[0] += q;
-            sum[1] = fmaf(q, xh, sum[1]);
-            dw[k][i] = fmaf(gy, xh, dw[k][i]);
-            if constexpr (BIAS) db[k][i] += gy;
+          for (int i = 0; i < M; ++i) {
+            const F q = vmul(yv[i], wv[i]), xh = vmul(vadd(sv[i], off), vset<F>(r));
+            acc0 = vadd(acc0, q);
+            acc1 = vfma(q, xh, acc1);
+            dw[k][i] = vfma(yv[i], xh, dw[k][i]);
+            if constexpr (BIAS) db[k][i] = vadd(db[k][i], yv[i]);
           }
         }
       }
     }
+    float sum[2] = {total(acc0), total(acc1)};
     group_sum(sum, group, s_sum, turn);
     const float c1 = p.rms ? 0.f : sum[0] * over, c2 = sum[1] * over;
     if (live) {
@@ -245,55 +335,207 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
         const int c = (k * group + j) * VE;
         if (c < p.D) {
           Row<float, VE> w;
-          load(w, p.weight, c);
-          Row<IO, VE> dx;
-          Row<RES, VE> dr;
+          F wv[M], sv[M], yv[M];
+          w.load(p.weight, c);
+          w.get(wv);
+          s[k].get(sv);
+          g[k].get(yv);
 #pragma unroll
-          for (int i = 0; i < VE; ++i) {
-            const float q = io_to_float<IO>(g[k].v[i]) * w.v[i], xh = (io_to_float<RES>(s[k].v[i]) - m) * r;
-            float ds = r * (q - c1 - xh * c2);
-            if (p.dresidual_out != nullptr) ds += io_to_float<RES>(add[k].v[i]);
-            dx.v[i] = float_to_io<IO>(ds);
-            dr.v[i] = float_to_io<RES>(ds);
+          for (int i = 0; i < M; ++i) {
+            const F xh = vmul(vadd(sv[i], off), vset<F>(r));
+            sv[i] = vfma(vmul(yv[i], wv[i]), vset<F>(r), vfma(xh, vset<F>(-r * c2), vset<F>(-r * c1)));
           }
-          store(dx, p.dx, here * p.D + c);
-          if (p.dresidual != nullptr) store(dr, p.dresidual, here * p.D + c);
+          if (p.dresidual_out != nullptr) {
+            F av[M];
+            add[k].get(av);
+#pragma unroll
+            for (int i = 0; i < M; ++i) sv[i] = vadd(sv[i], av[i]);
+          }
+          Row<IO, VE> dx;
+          dx.set(sv);
+          dx.store(p.dx, here * p.D + c);
+          if (p.dresidual != nullptr) {
+            Row<RES, VE> dr;
+            dr.set(sv);
+            dr.store(p.dresidual, here * p.D + c);
+          }
         }
       }
     }
   }
-  auto put = [&](float* out, auto& v) {                  // the block's sum of the groups' v
-    if (groups == 1) {
+  block_parts<VE, NV>(p.dw_part + (size_t)blockIdx.x * p.D, dw, p.D, group, s_part);
+  if constexpr (BIAS) block_parts<VE, NV>(p.db_part + (size_t)blockIdx.x * p.D, db, p.D, group, s_part);
+}
+
+// ------------------------------------------------------------------------------------------------- rows through a ring
+// The same for rows of whole 16 bytes, whose blocks stay on their SM and take tiles of rows one grid apart.  A tile is one
+// piece of memory in each tensor, and a bulk copy brings it to shared memory `stages` tiles ahead, which keeps enough bytes under
+// way without a register for them.
+__device__ __forceinline__ unsigned shared_address(const void* q) { return (unsigned)__cvta_generic_to_shared(q); }
+__device__ __forceinline__ void bulk_load(const void* dst, const void* src, unsigned bytes, const uint64_t* barrier) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_address(dst)), "l"(src), "r"(bytes),
+               "r"(shared_address(barrier))
+               : "memory");
+}
+__device__ __forceinline__ void expect(const uint64_t* barrier, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
+}
+// Waits for a tile.  Its copies are under way when the wait begins, so that it ends; the limit (seconds) is for a fault elsewhere.
+constexpr int kWaitLimit = 1 << 20;
+__device__ __forceinline__ bool wait_full(const uint64_t* barrier, unsigned phase) {
+  for (int i = 0; i < kWaitLimit; ++i) {
+    unsigned done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done)
+                 : "r"(shared_address(barrier)), "r"(phase)
+                 : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+constexpr int kMostStages = 4;
+
+// (columns and sums as in ssm_norm_rows_bwd_kernel)
+template <typename IO, typename RES, int VE, int NV, bool BIAS>
+__global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(const NormParams p, int stages) {
+  __shared__ float s_sum[2][kMaxWarps][2];
+  __shared__ uint64_t s_full[kMostStages];
+  extern __shared__ __align__(128) char s_ring[];
+  const int group = p.group, j = threadIdx.x % group, g = threadIdx.x / group;
+  const int rows = blockDim.x / group;
+  const bool add = p.dresidual_out != nullptr;
+  const int64_t tiles = (p.rows + rows - 1) / rows;
+  const int sbytes = rows * p.D * (int)sizeof(RES), ybytes = rows * p.D * (int)sizeof(IO), bytes = sbytes + ybytes + (add ? sbytes : 0);
+  if (threadIdx.x == 0)
+    for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&s_full[i])) : "memory");
+  __syncthreads();
+  dependency_wait();
+  auto fill = [&](int64_t tile, int stage) {               // thread 0
+    if (tile >= tiles) return;
+    const int64_t row = tile * rows;
+    const unsigned n = (unsigned)(p.rows - row < rows ? p.rows - row : rows) * p.D;
+    char* dst = s_ring + stage * bytes;
+    expect(&s_full[stage], n * (unsigned)(sizeof(IO) + (add ? 2 : 1) * sizeof(RES)));
+    bulk_load(dst, static_cast<const RES*>(p.s) + row * p.D, n * (unsigned)sizeof(RES), &s_full[stage]);
+    bulk_load(dst + sbytes, static_cast<const IO*>(p.dy) + row * p.D, n * (unsigned)sizeof(IO), &s_full[stage]);
+    if (add) bulk_load(dst + sbytes + ybytes, static_cast<const RES*>(p.dresidual_out) + row * p.D, n * (unsigned)sizeof(RES), &s_full[stage]);
+  };
+  if (threadIdx.x == 0)
+    for (int i = 0; i < stages - 1; ++i) fill(blockIdx.x + (int64_t)i * gridDim.x, i);
+  using F = Val<VE>;
+  constexpr int M = kVals<VE>;
+  F dw[NV][M], db[BIAS ? NV : 1][M];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      dw[k][i] = vset<F>(0.f);
+      if constexpr (BIAS) db[k][i] = vset<F>(0.f);
+    }
+  int stage = 0, turn = 0;
+  unsigned phase = 0;
+  const float over = 1.f / (float)p.D;
+  float mn = 0.f, rn = 0.f;
+  auto stats = [&](int64_t row) {
+    if (row < p.rows) {
+      mn = p.stats[2 * row];
+      rn = p.stats[2 * row + 1];
+    }
+  };
+  stats((int64_t)blockIdx.x * rows + g);
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+    const int64_t here = tile * rows + g;
+    const bool live = here < p.rows;
+    const float m = mn, r = rn;
+    stats(here + (int64_t)gridDim.x * rows);
+    const char* at = s_ring + stage * bytes;
+    const RES* bs = reinterpret_cast<const RES*>(at) + g * p.D;
+    const IO* by = reinterpret_cast<const IO*>(at + sbytes) + g * p.D;
+    const RES* ba = reinterpret_cast<const RES*>(at + sbytes + ybytes) + g * p.D;
+    const bool there = wait_full(&s_full[stage], phase);
+    const F off = vset<F>(-m);
+    F acc0 = vset<F>(there ? 0.f : NAN), acc1 = acc0;
+    if (live) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
+        if (c < p.D) {
+          Row<float, VE> w;
+          Row<RES, VE> s;
+          Row<IO, VE> y;
+          F wv[M], sv[M], yv[M];
+          w.load(p.weight, c);
+          w.get(wv);
+          s.load(bs, c);
+          s.get(sv);
+          y.load(by, c);
+          y.get(yv);
 #pragma unroll
-        for (int i = 0; i < VE; ++i)
-          if (c + i < p.D) out[c + i] = v[k][i];
+          for (int i = 0; i < M; ++i) {
+            const F q = vmul(yv[i], wv[i]), xh = vmul(vadd(sv[i], off), vset<F>(r));
+            acc0 = vadd(acc0, q);
+            acc1 = vfma(q, xh, acc1);
+            dw[k][i] = vfma(yv[i], xh, dw[k][i]);
+            if constexpr (BIAS) db[k][i] = vadd(db[k][i], yv[i]);
+          }
+        }
       }
-      return;
     }
-    __syncthreads();
+    if (group <= 32) __syncthreads();                      // (otherwise group_sum has one)
+    float sum[2] = {total(acc0), total(acc1)};
+    group_sum(sum, group, s_sum, turn);
+    // every thread is past the tile before this one
+    if (threadIdx.x == 0) fill(tile + (int64_t)(stages - 1) * gridDim.x, stage == 0 ? stages - 1 : stage - 1);
+    const float c1 = p.rms ? (there ? 0.f : NAN) : sum[0] * over, c2 = sum[1] * over;
+    if (live) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int c = (k * group + j) * VE;
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * group + j) * VE;
+        if (c < p.D) {
+          Row<float, VE> w;
+          Row<RES, VE> s;
+          Row<IO, VE> y;
+          F wv[M], sv[M], yv[M];
+          w.load(p.weight, c);
+          w.get(wv);
+          s.load(bs, c);
+          s.get(sv);
+          y.load(by, c);
+          y.get(yv);
 #pragma unroll
-      for (int i = 0; i < VE; ++i)
-        if (c + i < p.D) s_part[threadIdx.x / group * p.D + c + i] = v[k][i];
+          for (int i = 0; i < M; ++i) {
+            const F xh = vmul(vadd(sv[i], off), vset<F>(r));
+            sv[i] = vfma(vmul(yv[i], wv[i]), vset<F>(r), vfma(xh, vset<F>(-r * c2), vset<F>(-r * c1)));
+          }
+          if (add) {
+            F av[M];
+            s.load(ba, c);
+            s.get(av);
+#pragma unroll
+            for (int i = 0; i < M; ++i) sv[i] = vadd(sv[i], av[i]);
+          }
+          Row<IO, VE> dx;
+          dx.set(sv);
+          dx.store(p.dx, here * p.D + c);
+          if (p.dresidual != nullptr) {
+            Row<RES, VE> dr;
+            dr.set(sv);
+            dr.store(p.dresidual, here * p.D + c);
+          }
+        }
+      }
     }
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.D; c += blockDim.x) {
-      float a = s_part[c];
-      for (int q = 1; q < groups; ++q) a += s_part[q * p.D + c];
-      out[c] = a;
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1;
     }
-  };
-  put(p.dw_part + (size_t)blockIdx.x * p.D, dw);
-  if constexpr (BIAS) put(p.db_part + (size_t)blockIdx.x * p.D, db);
+  }
+  block_parts<VE, NV>(p.dw_part + (size_t)blockIdx.x * p.D, dw, p.D, group, reinterpret_cast<float*>(s_ring));
+  if constexpr (BIAS) block_parts<VE, NV>(p.db_part + (size_t)blockIdx.x * p.D, db, p.D, group, reinterpret_cast<float*>(s_ring));
 }
 
 // dweight and dbias from the blocks' parts, in a fixed order: 32 columns a block, its slices of threads take every kSlices-th part
-constexpr int kSlices = 8;
+constexpr int kSlices = 32;
 __global__ void __launch_bounds__(32 * kSlices) ssm_norm_parts_kernel(const float* __restrict__ dw_part, const float* __restrict__ db_part, int parts,
                                                                     int D, float* __restrict__ dw, float* __restrict__ db) {
   __shared__ float s_sum[kSlices][32];
@@ -303,14 +545,15 @@ __global__ void __launch_bounds__(32 * kSlices) ssm_norm_parts_kernel(const floa
   const float* part = blockIdx.y == 0 ? dw_part : db_part;
   float a = 0.f;
   if (d < D) {
-#pragma unroll 8
+#pragma unroll 10
     for (int q = slice; q < parts; q += kSlices) a += part[(size_t)q * D + d];
   }
   s_sum[slice][lane] = a;
   __syncthreads();
   if (slice == 0 && d < D) {
+    a = 0.f;
 #pragma unroll
-    for (int q = 1; q < kSlices; ++q) a += s_sum[q][lane];
+    for (int q = 0; q < kSlices; ++q) a += s_sum[q][lane];
     (blockIdx.y == 0 ? dw : db)[d] = a;
   }
 }
@@ -428,30 +671,51 @@ bool aligned(const void* q, size_t a) { return reinterpret_cast<uintptr_t>(q) % 
 int parts_of(const ssm_norm_problem_t& p) { return (int)(p.rows < kMaxParts ? p.rows : kMaxParts); }
 ssm_status_t status(cudaError_t e) { return e == cudaSuccess ? SSM_OK : SSM_ERR_CUDA; }
 
-// How a row is spread: NV vectors a thread, the fewest lanes idle, more vectors a thread where that is even.  0: it does not fit.
+// How a row is spread over a group: NV vectors a thread.  0: it does not fit.
 struct Spread {
   int nv, group;
 };
-constexpr int kMostNv = 4;
-Spread spread(int D, int VE, int (*most_threads)(int, int)) {
+int group_of(int vecs, int nv) {
+  int g = (vecs + nv - 1) / nv;
+  if (g > 32) return (g + 31) / 32 * 32;
+  while (g & (g - 1)) ++g;
+  return g;
+}
+// The most vectors a thread, of `most_nv` down, that leave no more than a tenth of the lanes idle beyond the least possible: the
+// sums over a group cost more the more warps it has (8192 x 5120 bf16 layer norm forward with 5, 4, 2, 1 vectors: 40, 45, 62, 93 us).
+Spread spread(int D, int VE, int most_nv, int (*most_threads)(int, int)) {
+  const int vecs = (D + VE - 1) / VE;
+  long long least = 0;
+  for (int pass = 0; pass < 2; ++pass)
+    for (int nv = most_nv; nv >= 1; --nv) {
+      const int g = group_of(vecs, nv);
+      if (g > most_threads(VE, nv)) continue;
+      const long long slots = (long long)nv * g;
+      if (pass == 0) least = least == 0 || slots < least ? slots : least;
+      else if (10 * slots <= 11 * least) return {nv, g};
+    }
+  return {0, 0};
+}
+// The ring's: the fewest vectors a thread, of those that leave the fewest lanes idle, with groups of at most 256 threads.
+Spread ring_spread(int D, int VE) {
   const int vecs = (D + VE - 1) / VE;
   Spread best{0, 0};
-  long long best_slots = 0;
-  for (int nv = kMostNv; nv >= 1; --nv) {
-    int g = (vecs + nv - 1) / nv;
-    if (g > 32) g = (g + 31) / 32 * 32;
-    else
-      while (g & (g - 1)) ++g;
-    if (g > most_threads(VE, nv)) continue;
-    const long long slots = (long long)nv * g;
-    if (best.nv == 0 || slots < best_slots) {
-      best = {nv, g};
-      best_slots = slots;
-    }
+  for (int nv = 1; nv <= 4; ++nv) {
+    const int g = group_of(vecs, nv);
+    if (g <= 256 && (best.nv == 0 || nv * g < best.nv * best.group)) best = {nv, g};
   }
   return best;
 }
 int block_threads(int group) { return group > 32 ? group : 128; }
+
+// Tiles of a ring of one block: at least two, and for as many blocks of an SM (eight at most) as then fit.  0: it does not fit.
+constexpr int kSharedBytes = 224 << 10;
+int ring_stages(size_t bytes) {
+  for (int blocks = 8; blocks >= 1; --blocks)
+    for (int n = kMostStages; n >= 2; --n)
+      if (blocks * (n * bytes + 2048) <= kSharedBytes) return n;
+  return 0;
+}
 
 template <typename IO, typename RES, int VE, int NV>
 cudaError_t launch_fwd_rows(const NormParams& p, cudaStream_t s) {
@@ -461,15 +725,37 @@ cudaError_t launch_fwd_rows(const NormParams& p, cudaStream_t s) {
 
 template <typename IO, typename RES, int VE>
 cudaError_t launch_fwd_ve(NormParams p, cudaStream_t s) {
-  const Spread sp = spread(p.D, VE, fwd_threads);
+  // (single elements of long rows: the kernel for long rows is faster, bf16 8192 x 2561 37 us against 52)
+  const Spread sp = VE == 1 && p.D > 2048 ? Spread{0, 0} : spread(p.D, VE, sizeof(IO) == sizeof(RES) ? 5 : 4, fwd_threads);
   p.group = sp.group;
   switch (sp.nv) {
     case 1: return launch_fwd_rows<IO, RES, VE, 1>(p, s);
     case 2: return launch_fwd_rows<IO, RES, VE, 2>(p, s);
     case 3: return launch_fwd_rows<IO, RES, VE, 3>(p, s);
     case 4: return launch_fwd_rows<IO, RES, VE, 4>(p, s);
+    case 5: return launch_fwd_rows<IO, RES, VE, 5>(p, s);
     default: return launch_dependent(ssm_norm_fwd_kernel<IO, RES>, (unsigned)p.rows, kNormThreads, 0, 1, s, p);
   }
+}
+
+template <typename IO, typename RES, int VE, int NV, bool BIAS>
+cudaError_t launch_bwd_ring(const NormParams& p, int* parts, bool* done, cudaStream_t s) {
+  const auto kernel = ssm_norm_ring_bwd_kernel<IO, RES, VE, NV, BIAS>;
+  const int threads = block_threads(p.group), rows = threads / p.group;
+  const size_t bytes = (size_t)rows * p.D * (sizeof(IO) + (p.dresidual_out != nullptr ? 2 : 1) * sizeof(RES));
+  const int stages = ring_stages(bytes);
+  *done = stages > 0;
+  if (!*done) return cudaSuccess;
+  const size_t smem = stages * bytes > rows * p.D * sizeof(float) ? stages * bytes : rows * p.D * sizeof(float);
+  KernelLimits lim;
+  const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), threads, smem, &lim);
+  if (e != cudaSuccess) return e;
+  const long long tiles = (p.rows + rows - 1) / rows, most = (long long)lim.sms * lim.per_sm;
+  const long long blocks = tiles < most ? tiles : most;
+  *parts = (int)(blocks < kMaxParts ? blocks : kMaxParts);
+  NormParams q = p;
+  if constexpr (BIAS) q.db_part = q.dw_part + (size_t)*parts * p.D;
+  return launch_dependent(kernel, (unsigned)*parts, threads, smem, 1, s, q, stages);
 }
 
 template <typename IO, typename RES, int VE, int NV, bool BIAS>
@@ -490,20 +776,35 @@ cudaError_t launch_bwd_rows(const NormParams& p, int* parts, cudaStream_t s) {
   return launch_dependent(kernel, (unsigned)blocks, threads, smem, 1, s, q);
 }
 template <typename IO, typename RES, int VE, int NV>
-cudaError_t launch_bwd_nv(const NormParams& p, bool bias, int* parts, cudaStream_t s) {
+cudaError_t launch_bwd_nv(const NormParams& p, bool bias, bool ring, int* parts, bool* done, cudaStream_t s) {
+  if constexpr (VE > 1) {
+    if (ring) return bias ? launch_bwd_ring<IO, RES, VE, NV, true>(p, parts, done, s) : launch_bwd_ring<IO, RES, VE, NV, false>(p, parts, done, s);
+  }
+  *done = true;
   return bias ? launch_bwd_rows<IO, RES, VE, NV, true>(p, parts, s) : launch_bwd_rows<IO, RES, VE, NV, false>(p, parts, s);
 }
 
+// Up to 192 threads of two vectors a row's next one waits in registers; where a row is longer the sums take so many that the ring
+// is faster (layer norm with bias, 8192 rows of bf16: 5120 columns 66 us against 97, 4096 64 against 74, 2560 45 against 40).
 template <typename IO, typename RES, int VE>
 cudaError_t launch_bwd_ve(NormParams p, bool bias, int* parts, cudaStream_t s) {
-  const Spread sp = spread(p.D, VE, bwd_threads);
-  p.group = sp.group;
-  switch (sp.nv) {
-    case 1: return launch_bwd_nv<IO, RES, VE, 1>(p, bias, parts, s);
-    case 2: return launch_bwd_nv<IO, RES, VE, 2>(p, bias, parts, s);
-    case 3: return launch_bwd_nv<IO, RES, VE, 3>(p, bias, parts, s);
-    case 4: return launch_bwd_nv<IO, RES, VE, 4>(p, bias, parts, s);
-    default: break;
+  bool ring = VE > 1 && p.D > 2 * 192 * VE;
+  Spread sp = ring ? ring_spread(p.D, VE) : spread(p.D, VE, VE > 1 ? 2 : 4, bwd_threads);
+  for (;;) {
+    p.group = sp.group;
+    bool done = false;
+    cudaError_t e = cudaSuccess;
+    switch (sp.nv) {
+      case 1: e = launch_bwd_nv<IO, RES, VE, 1>(p, bias, ring, parts, &done, s); break;
+      case 2: e = launch_bwd_nv<IO, RES, VE, 2>(p, bias, ring, parts, &done, s); break;
+      case 3: e = launch_bwd_nv<IO, RES, VE, 3>(p, bias, ring, parts, &done, s); break;
+      case 4: e = launch_bwd_nv<IO, RES, VE, 4>(p, bias, ring, parts, &done, s); break;
+      default: break;
+    }
+    if (done || e != cudaSuccess) return e;
+    if (!ring) break;
+    ring = false;                                          // (does not fit the ring)
+    sp = spread(p.D, VE, 4, bwd_threads);
   }
   *parts = (int)(p.rows < kMaxParts ? p.rows : kMaxParts);
   p.rows_per_part = (int)((p.rows + *parts - 1) / *parts);
