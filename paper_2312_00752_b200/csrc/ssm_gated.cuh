@@ -11,7 +11,7 @@
 namespace ssm {
 
 constexpr int kGatedSteps = 8;     // steps between two saved states
-constexpr int kGatedCluster = 8;   // blocks of a cluster at most
+constexpr int kGatedCluster = 16;  // blocks of a cluster at most
 
 struct GatedParams {
   const void* x;
@@ -223,6 +223,20 @@ __device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
 }
 
+
+// Launches `kernel` with clusters of `c` blocks.  More than eight need the kernel's leave, and where a device has no room for
+// them eight it is; *c: what it came to.
+template <typename Kernel>
+inline cudaError_t launch_gated(Kernel kernel, long long groups, int threads, size_t smem, int* c, cudaStream_t s, const GatedParams& p) {
+  if (*c > 8) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = launch_dependent(kernel, (unsigned)(groups * *c), threads, smem, *c, s, p);
+    if (e == cudaSuccess) return e;
+    (void)cudaGetLastError();
+    *c = 8;
+  }
+  return launch_dependent(kernel, (unsigned)(groups * *c), threads, smem, *c, s, p);
+}
 #endif
 
 // ------------------------------------------------------------------------------------------------------------ launches
@@ -231,7 +245,7 @@ __device__ __forceinline__ void cp_async4(void* dst, const void* src, bool valid
 cudaError_t launch_gated_fwd(const GatedParams& p, int io_dtype, bool decay, int unit, cudaStream_t s);
 // parts: how many rows of dA_part were written
 cudaError_t launch_gated_bwd(const GatedParams& p, int io_dtype, bool decay, int unit, int* parts, cudaStream_t s);
-// Blocks that share the tiles of a group of channels: `rounds(c)` of a tile each, `tiles` groups, `resident` blocks at once.
-int choose_gated_cluster(long long tiles, long long steps, int tile_steps, long long resident);
+// Blocks of a cluster that shares the tiles (of `tile_steps` each) of a group of channels; `groups` of them, `resident` blocks at once.
+int choose_gated_cluster(long long groups, long long steps, int tile_steps, long long resident);
 
 }  // namespace ssm

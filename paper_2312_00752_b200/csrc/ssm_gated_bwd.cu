@@ -323,9 +323,10 @@ cudaError_t launch(GatedParams p, int* parts, cudaStream_t s) {
   const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), 32 * W, smem, &lim);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.tiles * p.batch;
-  const int c = choose_gated_cluster(tiles, p.L, kTile, (long long)lim.sms * lim.per_sm);
+  int c = choose_gated_cluster(tiles, p.L, kTile, (long long)lim.sms * lim.per_sm);
+  const cudaError_t launched = launch_gated(kernel, tiles, 32 * W, smem, &c, s, p);
   *parts = p.batch * c;
-  return launch_dependent(kernel, (unsigned)(tiles * c), 32 * W, smem, c, s, p);
+  return launched;
 }
 
 template <typename IO, class F, int COPY>
