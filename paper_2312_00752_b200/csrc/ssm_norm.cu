@@ -51,15 +51,34 @@ struct Row {   // VE elements of type T as they lie in memory
   using Word = typename std::conditional<VE == 1, T, uint4>::type;
   static constexpr int kWords = VE == 1 ? 1 : VE * (int)sizeof(T) / 16;
   Word w[kWords];
+  // Global memory; 32 bytes move at once: two accesses of 16 would each touch every second 16 bytes of the lines, and the float32
+  // parameters of bf16 rows were what the L1's data path spent most of its time on (8192 x 5120 layer norm forward 41 us, XX so).
   __device__ __forceinline__ void load(const void* base, int64_t at) {
     const Word* q = reinterpret_cast<const Word*>(static_cast<const T*>(base) + at);
+    if constexpr (VE > 1 && kWords == 2) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[1].x), "=r"(w[1].y), "=r"(w[1].z), "=r"(w[1].w)
+                   : "l"(q));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = q[i];
+    }
+  }
+  __device__ __forceinline__ void load_shared(const T* base, int at) {
+    const Word* q = reinterpret_cast<const Word*>(base + at);
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = q[i];
   }
   __device__ __forceinline__ void store(void* base, int64_t at) const {
     Word* q = reinterpret_cast<Word*>(static_cast<T*>(base) + at);
+    if constexpr (VE > 1 && kWords == 2) {
+      asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(w[0].x), "r"(w[0].y), "r"(w[0].z), "r"(w[0].w), "r"(w[1].x),
+                   "r"(w[1].y), "r"(w[1].z), "r"(w[1].w), "l"(q)
+                   : "memory");
+    } else {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) q[i] = w[i];
+      for (int i = 0; i < kWords; ++i) q[i] = w[i];
+    }
   }
   __device__ __forceinline__ void get(Val<VE> (&v)[kVals<VE>]) const {
     if constexpr (VE == 1) {
@@ -466,9 +485,9 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
           F wv[M], sv[M], yv[M];
           w.load(p.weight, c);
           w.get(wv);
-          s.load(bs, c);
+          s.load_shared(bs, c);
           s.get(sv);
-          y.load(by, c);
+          y.load_shared(by, c);
           y.get(yv);
 #pragma unroll
           for (int i = 0; i < M; ++i) {
@@ -498,9 +517,9 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
           F wv[M], sv[M], yv[M];
           w.load(p.weight, c);
           w.get(wv);
-          s.load(bs, c);
+          s.load_shared(bs, c);
           s.get(sv);
-          y.load(by, c);
+          y.load_shared(by, c);
           y.get(yv);
 #pragma unroll
           for (int i = 0; i < M; ++i) {
@@ -509,7 +528,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
           }
           if (add) {
             F av[M];
-            s.load(ba, c);
+            s.load_shared(ba, c);
             s.get(av);
 #pragma unroll
             for (int i = 0; i < M; ++i) sv[i] = vadd(sv[i], av[i]);
@@ -814,23 +833,24 @@ cudaError_t launch_bwd_ve(NormParams p, bool bias, int* parts, cudaStream_t s) {
   return launch_dependent(ssm_norm_params_kernel<IO, RES>, dim3((p.D + kNormThreads - 1) / kNormThreads, *parts), kNormThreads, 0, 1, s, p);
 }
 
-// whether rows are whole 16 bytes at aligned pointers
-template <typename IO>
+// whether rows are whole 16 bytes of io, at pointers that are aligned to an access: 16 bytes, 32 where a float32 goes with a bf16
+template <typename IO, typename RES>
 bool wide(const NormParams& p) {
   uintptr_t bits = (uintptr_t)p.D * sizeof(IO);
-  for (const void* q : {p.x, p.residual, (const void*)p.weight, (const void*)p.bias, (const void*)p.y, (const void*)p.residual_out, p.s, p.dy,
-                        p.dresidual_out, (const void*)p.dx, (const void*)p.dresidual})
-    bits |= reinterpret_cast<uintptr_t>(q);
+  for (const void* q : {p.x, (const void*)p.y, p.dy, (const void*)p.dx}) bits |= reinterpret_cast<uintptr_t>(q);
+  for (const void* q : {p.residual, (const void*)p.residual_out, p.s, p.dresidual_out, (const void*)p.dresidual})
+    bits |= reinterpret_cast<uintptr_t>(q) * sizeof(IO) / sizeof(RES);
+  for (const void* q : {(const void*)p.weight, (const void*)p.bias}) bits |= reinterpret_cast<uintptr_t>(q) * sizeof(IO) / sizeof(float);
   return bits % 16 == 0;
 }
 
 template <typename IO, typename RES>
 cudaError_t launch_forward(const NormParams& p, cudaStream_t s) {
-  return wide<IO>(p) ? launch_fwd_ve<IO, RES, 16 / sizeof(IO)>(p, s) : launch_fwd_ve<IO, RES, 1>(p, s);
+  return wide<IO, RES>(p) ? launch_fwd_ve<IO, RES, 16 / sizeof(IO)>(p, s) : launch_fwd_ve<IO, RES, 1>(p, s);
 }
 template <typename IO, typename RES>
 cudaError_t launch_backward(const NormParams& p, bool bias, int* parts, cudaStream_t s) {
-  return wide<IO>(p) ? launch_bwd_ve<IO, RES, 16 / sizeof(IO)>(p, bias, parts, s) : launch_bwd_ve<IO, RES, 1>(p, bias, parts, s);
+  return wide<IO, RES>(p) ? launch_bwd_ve<IO, RES, 16 / sizeof(IO)>(p, bias, parts, s) : launch_bwd_ve<IO, RES, 1>(p, bias, parts, s);
 }
 
 }  // namespace
