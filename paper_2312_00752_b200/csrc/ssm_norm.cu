@@ -263,7 +263,7 @@ __device__ __forceinline__ void block_parts(float* __restrict__ out, const Val<V
 // Rows blockIdx.x (blockDim.x / group) + .., one grid of groups apart; the thread's columns stay the same, so dweight and dbias are
 // summed in registers over all its rows, then over the groups of the block in order, and written as one part per block.  The next
 // row is loaded before this one is reduced.
-template <typename IO, typename RES, int VE, int NV, bool BIAS>
+template <typename IO, typename RES, int VE, int NV, bool BIAS, bool FULL>
 __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(const NormParams p) {
   __shared__ float s_sum[2][kMaxWarps][2];
   extern __shared__ float s_part[];                      // groups of 32 threads or fewer: [groups][D]
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) {
+        if (FULL || c < p.D) {
           sn[k].load(p.s, row * p.D + c);
           gn[k].load(p.dy, row * p.D + c);
         }
@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) add[k].load(p.dresidual_out, here * p.D + c);
+        if (FULL || c < p.D) add[k].load(p.dresidual_out, here * p.D + c);
       }
     }
     fetch(here + apart);
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) {
+        if (FULL || c < p.D) {
           Row<float, VE> w;
           F wv[M], sv[M], yv[M];
           w.load(p.weight, c);
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) {
+        if (FULL || c < p.D) {
           Row<float, VE> w;
           F wv[M], sv[M], yv[M];
           w.load(p.weight, c);
@@ -415,7 +415,7 @@ __device__ __forceinline__ bool wait_full(const uint64_t* barrier, unsigned phas
 constexpr int kMostStages = 4;
 
 // (columns and sums as in ssm_norm_rows_bwd_kernel)
-template <typename IO, typename RES, int VE, int NV, bool BIAS>
+template <typename IO, typename RES, int VE, int NV, bool BIAS, bool FULL>
 __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(const NormParams p, int stages) {
   __shared__ float s_sum[2][kMaxWarps][2];
   __shared__ uint64_t s_full[kMostStages];
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) {
+        if (FULL || c < p.D) {
           Row<float, VE> w;
           Row<RES, VE> s;
           Row<IO, VE> y;
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
-        if (c < p.D) {
+        if (FULL || c < p.D) {
           Row<float, VE> w;
           Row<RES, VE> s;
           Row<IO, VE> y;
@@ -725,6 +725,9 @@ Spread ring_spread(int D, int VE) {
   }
   return best;
 }
+// no lane of the group idle: the backward kernels go without their tests of columns (3 to 5 %; the forward one keeps them, it
+// holds the parameters in registers too early without: 8192 x 5120 42 us against 36)
+bool even(const NormParams& p, int VE, int NV) { return p.D == NV * p.group * VE; }
 int block_threads(int group) { return group > 32 ? group : 128; }
 
 // Tiles of a ring of one block: at least two, and for as many blocks of an SM (eight at most) as then fit.  0: it does not fit.
@@ -739,7 +742,8 @@ int ring_stages(size_t bytes) {
 template <typename IO, typename RES, int VE, int NV>
 cudaError_t launch_fwd_rows(const NormParams& p, cudaStream_t s) {
   const int threads = block_threads(p.group), rows = threads / p.group;
-  return launch_dependent(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV>, (unsigned)((p.rows + rows - 1) / rows), threads, 0, 1, s, p);
+  const unsigned blocks = (unsigned)((p.rows + rows - 1) / rows);
+  return launch_dependent(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV>, blocks, threads, 0, 1, s, p);
 }
 
 template <typename IO, typename RES, int VE>
@@ -759,7 +763,7 @@ cudaError_t launch_fwd_ve(NormParams p, cudaStream_t s) {
 
 template <typename IO, typename RES, int VE, int NV, bool BIAS>
 cudaError_t launch_bwd_ring(const NormParams& p, int* parts, bool* done, cudaStream_t s) {
-  const auto kernel = ssm_norm_ring_bwd_kernel<IO, RES, VE, NV, BIAS>;
+  const auto kernel = even(p, VE, NV) ? ssm_norm_ring_bwd_kernel<IO, RES, VE, NV, BIAS, true> : ssm_norm_ring_bwd_kernel<IO, RES, VE, NV, BIAS, false>;
   const int threads = block_threads(p.group), rows = threads / p.group;
   const size_t bytes = (size_t)rows * p.D * (sizeof(IO) + (p.dresidual_out != nullptr ? 2 : 1) * sizeof(RES));
   const int stages = ring_stages(bytes);
@@ -779,7 +783,7 @@ cudaError_t launch_bwd_ring(const NormParams& p, int* parts, bool* done, cudaStr
 
 template <typename IO, typename RES, int VE, int NV, bool BIAS>
 cudaError_t launch_bwd_rows(const NormParams& p, int* parts, cudaStream_t s) {
-  const auto kernel = ssm_norm_rows_bwd_kernel<IO, RES, VE, NV, BIAS>;
+  const auto kernel = even(p, VE, NV) ? ssm_norm_rows_bwd_kernel<IO, RES, VE, NV, BIAS, true> : ssm_norm_rows_bwd_kernel<IO, RES, VE, NV, BIAS, false>;
   const int threads = block_threads(p.group), rows = threads / p.group;
   const size_t smem = rows > 1 ? 128 * VE * NV * sizeof(float) : 0;     // rows p.D at most
   KernelLimits lim;
