@@ -38,7 +38,7 @@ struct NormParams {
 
 // ------------------------------------------------------------------------------------------------------ rows in registers
 // A group of threads holds a row: NV vectors of VE adjacent elements a thread, vector k of thread j at (k group + j) VE, so that the
-// group's accesses are contiguous.  VE is 16 bytes of io, or one element where the rows do not allow such accesses.
+// group's accesses are contiguous.  VE is 16 bytes of io, a pair of bf16 or one element, as the rows allow.
 template <int VE>
 using Val = typename std::conditional<VE == 1, float, float2>::type;   // what arithmetic is done on
 template <int VE>
@@ -48,8 +48,9 @@ __device__ __forceinline__ float total(float2 v) { return v.x + v.y; }
 
 template <typename T, int VE>
 struct Row {   // VE elements of type T as they lie in memory
-  using Word = typename std::conditional<VE == 1, T, uint4>::type;
-  static constexpr int kWords = VE == 1 ? 1 : VE * (int)sizeof(T) / 16;
+  static constexpr int kBytes = VE * (int)sizeof(T);
+  using Word = typename std::conditional<VE == 1, T, typename std::conditional<kBytes == 4, uint32_t, typename std::conditional<kBytes == 8, uint2, uint4>::type>::type>::type;
+  static constexpr int kWords = kBytes <= 16 ? 1 : kBytes / 16;
   Word w[kWords];
   // Global memory; 32 bytes move at once: two accesses of 16 would each touch every second 16 bytes of the lines, and the float32
   // parameters of bf16 rows were what the L1's data path spent most of its time on (8192 x 5120 layer norm forward 41 us, XX so).
@@ -83,6 +84,10 @@ struct Row {   // VE elements of type T as they lie in memory
   __device__ __forceinline__ void get(Val<VE> (&v)[kVals<VE>]) const {
     if constexpr (VE == 1) {
       v[0] = io_to_float<T>(w[0]);
+    } else if constexpr (kBytes == 4) {
+      v[0] = make_float2(bf16lo(w[0]), bf16hi(w[0]));
+    } else if constexpr (kBytes == 8) {
+      v[0] = make_float2(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
     } else {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) {
@@ -100,6 +105,11 @@ struct Row {   // VE elements of type T as they lie in memory
   __device__ __forceinline__ void set(const Val<VE> (&v)[kVals<VE>]) {   // rounded to T
     if constexpr (VE == 1) {
       w[0] = float_to_io<T>(v[0]);
+    } else if constexpr (kBytes == 4) {
+      const __nv_bfloat162 c = __floats2bfloat162_rn(v[0].x, v[0].y);
+      w[0] = *reinterpret_cast<const uint32_t*>(&c);
+    } else if constexpr (kBytes == 8) {
+      w[0] = make_uint2(__float_as_uint(v[0].x), __float_as_uint(v[0].y));
     } else {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) {
@@ -123,7 +133,7 @@ constexpr int kMaxWarps = 32;
 // threads of a block, by vectors a thread: what the registers allow
 constexpr int fwd_threads(int VE, int NV) { return VE * NV > 48 ? 384 : VE * NV > 16 ? 512 : 1024; }
 constexpr int bwd_threads(int VE, int NV) {
-  if (VE == 1) return 768;
+  if (VE <= 2) return NV == 8 ? 512 : 768;
   if (VE == 4) return NV == 1 ? 1024 : NV == 2 ? 640 : 384;
   return NV == 1 ? 768 : NV == 2 ? 384 : 256;
 }
@@ -706,7 +716,8 @@ Spread spread(int D, int VE, int most_nv, int (*most_threads)(int, int)) {
   const int vecs = (D + VE - 1) / VE;
   long long least = 0;
   for (int pass = 0; pass < 2; ++pass)
-    for (int nv = most_nv; nv >= 1; --nv) {
+    for (int nv : {8, 5, 4, 3, 2, 1}) {
+      if (nv > most_nv || (nv == 5 && most_threads == bwd_threads)) continue;
       const int g = group_of(vecs, nv);
       if (g > most_threads(VE, nv)) continue;
       const long long slots = (long long)nv * g;
@@ -749,7 +760,7 @@ cudaError_t launch_fwd_rows(const NormParams& p, cudaStream_t s) {
 template <typename IO, typename RES, int VE>
 cudaError_t launch_fwd_ve(NormParams p, cudaStream_t s) {
   // (single elements of long rows: the kernel for long rows is faster, bf16 8192 x 2561 37 us against 52)
-  const Spread sp = VE == 1 && p.D > 2048 ? Spread{0, 0} : spread(p.D, VE, sizeof(IO) == sizeof(RES) ? 5 : 4, fwd_threads);
+  const Spread sp = VE == 1 && p.D > 2048 ? Spread{0, 0} : spread(p.D, VE, VE <= 2 ? 8 : sizeof(IO) == sizeof(RES) ? 5 : 4, fwd_threads);
   p.group = sp.group;
   switch (sp.nv) {
     case 1: return launch_fwd_rows<IO, RES, VE, 1>(p, s);
@@ -757,6 +768,9 @@ cudaError_t launch_fwd_ve(NormParams p, cudaStream_t s) {
     case 3: return launch_fwd_rows<IO, RES, VE, 3>(p, s);
     case 4: return launch_fwd_rows<IO, RES, VE, 4>(p, s);
     case 5: return launch_fwd_rows<IO, RES, VE, 5>(p, s);
+    case 8:
+      if constexpr (VE <= 2) return launch_fwd_rows<IO, RES, VE, 8>(p, s);
+      [[fallthrough]];
     default: return launch_dependent(ssm_norm_fwd_kernel<IO, RES>, (unsigned)p.rows, kNormThreads, 0, 1, s, p);
   }
 }
@@ -800,7 +814,7 @@ cudaError_t launch_bwd_rows(const NormParams& p, int* parts, cudaStream_t s) {
 }
 template <typename IO, typename RES, int VE, int NV>
 cudaError_t launch_bwd_nv(const NormParams& p, bool bias, bool ring, int* parts, bool* done, cudaStream_t s) {
-  if constexpr (VE > 1) {
+  if constexpr (VE > 2) {
     if (ring) return bias ? launch_bwd_ring<IO, RES, VE, NV, true>(p, parts, done, s) : launch_bwd_ring<IO, RES, VE, NV, false>(p, parts, done, s);
   }
   *done = true;
@@ -811,8 +825,8 @@ cudaError_t launch_bwd_nv(const NormParams& p, bool bias, bool ring, int* parts,
 // is faster (layer norm with bias, 8192 rows of bf16: 5120 columns 66 us against 97, 4096 64 against 74, 2560 45 against 40).
 template <typename IO, typename RES, int VE>
 cudaError_t launch_bwd_ve(NormParams p, bool bias, int* parts, cudaStream_t s) {
-  bool ring = VE > 1 && p.D > 2 * 192 * VE;
-  Spread sp = ring ? ring_spread(p.D, VE) : spread(p.D, VE, VE > 1 ? 2 : 4, bwd_threads);
+  bool ring = VE > 2 && p.D > 2 * 192 * VE;
+  Spread sp = ring ? ring_spread(p.D, VE) : spread(p.D, VE, VE <= 2 ? 8 : 2, bwd_threads);
   for (;;) {
     p.group = sp.group;
     bool done = false;
@@ -822,6 +836,9 @@ cudaError_t launch_bwd_ve(NormParams p, bool bias, int* parts, cudaStream_t s) {
       case 2: e = launch_bwd_nv<IO, RES, VE, 2>(p, bias, ring, parts, &done, s); break;
       case 3: e = launch_bwd_nv<IO, RES, VE, 3>(p, bias, ring, parts, &done, s); break;
       case 4: e = launch_bwd_nv<IO, RES, VE, 4>(p, bias, ring, parts, &done, s); break;
+      case 8:
+        if constexpr (VE <= 2) e = launch_bwd_nv<IO, RES, VE, 8>(p, bias, ring, parts, &done, s);
+        break;
       default: break;
     }
     if (done || e != cudaSuccess) return e;
@@ -837,24 +854,31 @@ cudaError_t launch_bwd_ve(NormParams p, bool bias, int* parts, cudaStream_t s) {
   return launch_dependent(ssm_norm_params_kernel<IO, RES>, dim3((p.D + kNormThreads - 1) / kNormThreads, *parts), kNormThreads, 0, 1, s, p);
 }
 
-// whether rows are whole 16 bytes of io, at pointers that are aligned to an access: 16 bytes, 32 where a float32 goes with a bf16
+// Whether rows are whole `bytes` of io, at pointers that are aligned to an access: so many bytes, twice as many where a float32
+// goes with a bf16.
 template <typename IO, typename RES>
-bool wide(const NormParams& p) {
+bool whole(const NormParams& p, int bytes) {
   uintptr_t bits = (uintptr_t)p.D * sizeof(IO);
   for (const void* q : {p.x, (const void*)p.y, p.dy, (const void*)p.dx}) bits |= reinterpret_cast<uintptr_t>(q);
   for (const void* q : {p.residual, (const void*)p.residual_out, p.s, p.dresidual_out, (const void*)p.dresidual})
     bits |= reinterpret_cast<uintptr_t>(q) * sizeof(IO) / sizeof(RES);
   for (const void* q : {(const void*)p.weight, (const void*)p.bias}) bits |= reinterpret_cast<uintptr_t>(q) * sizeof(IO) / sizeof(float);
-  return bits % 16 == 0;
+  return bits % bytes == 0;
 }
 
 template <typename IO, typename RES>
 cudaError_t launch_forward(const NormParams& p, cudaStream_t s) {
-  return wide<IO, RES>(p) ? launch_fwd_ve<IO, RES, 16 / sizeof(IO)>(p, s) : launch_fwd_ve<IO, RES, 1>(p, s);
+  if (whole<IO, RES>(p, 16)) return launch_fwd_ve<IO, RES, 16 / sizeof(IO)>(p, s);
+  if constexpr (sizeof(IO) == 2)
+    if (whole<IO, RES>(p, 4)) return launch_fwd_ve<IO, RES, 2>(p, s);
+  return launch_fwd_ve<IO, RES, 1>(p, s);
 }
 template <typename IO, typename RES>
 cudaError_t launch_backward(const NormParams& p, bool bias, int* parts, cudaStream_t s) {
-  return wide<IO, RES>(p) ? launch_bwd_ve<IO, RES, 16 / sizeof(IO)>(p, bias, parts, s) : launch_bwd_ve<IO, RES, 1>(p, bias, parts, s);
+  if (whole<IO, RES>(p, 16)) return launch_bwd_ve<IO, RES, 16 / sizeof(IO)>(p, bias, parts, s);
+  if constexpr (sizeof(IO) == 2)
+    if (whole<IO, RES>(p, 4)) return launch_bwd_ve<IO, RES, 2>(p, bias, parts, s);
+  return launch_bwd_ve<IO, RES, 1>(p, bias, parts, s);
 }
 
 }  // namespace
