@@ -98,8 +98,10 @@ struct Feed {
   }
 };
 
+// Blocks of an SM: the decay form wants the registers of three ((2, 8192, 2560) bf16 84 us with four, 75 with three), with a
+// mask it is faster with four ((8, 2048, 2560) 84 us, 91 with three), as is the convex form.
 template <typename IO, class F, bool DECAY, bool RESET, int COPY>
-__global__ void __launch_bounds__(32 * W, 4) ssm_gated_fwd_kernel(const GatedParams p) {
+__global__ void __launch_bounds__(32 * W, DECAY && !RESET ? 3 : 4) ssm_gated_fwd_kernel(const GatedParams p) {
   using Io = Lane<IO, F>;
   using Raw = typename Io::Raw;
   using In = Feed<IO, F, DECAY, COPY>;
