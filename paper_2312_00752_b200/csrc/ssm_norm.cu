@@ -53,7 +53,7 @@ struct Row {   // VE elements of type T as they lie in memory
   static constexpr int kWords = kBytes <= 16 ? 1 : kBytes / 16;
   Word w[kWords];
   // Global memory; 32 bytes move at once: two accesses of 16 would each touch every second 16 bytes of the lines, and the float32
-  // parameters of bf16 rows were what the L1's data path spent most of its time on (8192 x 5120 layer norm forward 41 us, XX so).
+  // parameters of bf16 rows were what the L1's data path spent most of its time on (8192 x 5120 layer norm forward 41 us, 36 so).
   __device__ __forceinline__ void load(const void* base, int64_t at) {
     const Word* q = reinterpret_cast<const Word*>(static_cast<const T*>(base) + at);
     if constexpr (VE > 1 && kWords == 2) {
@@ -397,9 +397,8 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
 }
 
 // ------------------------------------------------------------------------------------------------- rows through a ring
-// The same for rows of whole 16 bytes, whose blocks stay on their SM and take tiles of rows one grid apart.  A tile is one
-// piece of memory in each tensor, and a bulk copy brings it to shared memory `stages` tiles ahead, which keeps enough bytes under
-// way without a register for them.
+// The same for long rows of whole 16 bytes, with the whole block on one row: its tensors are brought to shared memory `stages` rows
+// ahead, each by one bulk copy, which keeps enough bytes under way without a register for them.
 __device__ __forceinline__ unsigned shared_address(const void* q) { return (unsigned)__cvta_generic_to_shared(q); }
 __device__ __forceinline__ void bulk_load(const void* dst, const void* src, unsigned bytes, const uint64_t* barrier) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_address(dst)), "l"(src), "r"(bytes),
@@ -409,7 +408,8 @@ __device__ __forceinline__ void bulk_load(const void* dst, const void* src, unsi
 __device__ __forceinline__ void expect(const uint64_t* barrier, unsigned bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
 }
-// Waits for a tile.  Its copies are under way when the wait begins, so that it ends; the limit (seconds) is for a fault elsewhere.
+// Waits for a row.  Its copies are under way when the wait begins, so that it ends; the limit (seconds) is for a fault elsewhere,
+// and what would be made of the row is NaN then.
 constexpr int kWaitLimit = 1 << 20;
 __device__ __forceinline__ bool wait_full(const uint64_t* barrier, unsigned phase) {
   for (int i = 0; i < kWaitLimit; ++i) {
@@ -424,35 +424,30 @@ __device__ __forceinline__ bool wait_full(const uint64_t* barrier, unsigned phas
 }
 constexpr int kMostStages = 4;
 
-// (columns and sums as in ssm_norm_rows_bwd_kernel)
 template <typename IO, typename RES, int VE, int NV, bool BIAS, bool FULL>
 __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(const NormParams p, int stages) {
+  using F = Val<VE>;
+  constexpr int M = kVals<VE>;
   __shared__ float s_sum[2][kMaxWarps][2];
   __shared__ uint64_t s_full[kMostStages];
   extern __shared__ __align__(128) char s_ring[];
-  const int group = p.group, j = threadIdx.x % group, g = threadIdx.x / group;
-  const int rows = blockDim.x / group;
+  const int group = p.group, j = threadIdx.x;
   const bool add = p.dresidual_out != nullptr;
-  const int64_t tiles = (p.rows + rows - 1) / rows;
-  const int sbytes = rows * p.D * (int)sizeof(RES), ybytes = rows * p.D * (int)sizeof(IO), bytes = sbytes + ybytes + (add ? sbytes : 0);
+  const int sbytes = p.D * (int)sizeof(RES), ybytes = p.D * (int)sizeof(IO), bytes = sbytes + ybytes + (add ? sbytes : 0);
   if (threadIdx.x == 0)
     for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&s_full[i])) : "memory");
   __syncthreads();
   dependency_wait();
-  auto fill = [&](int64_t tile, int stage) {               // thread 0
-    if (tile >= tiles) return;
-    const int64_t row = tile * rows;
-    const unsigned n = (unsigned)(p.rows - row < rows ? p.rows - row : rows) * p.D;
+  auto fill = [&](int64_t row, int stage) {                // thread 0
+    if (row >= p.rows) return;
     char* dst = s_ring + stage * bytes;
-    expect(&s_full[stage], n * (unsigned)(sizeof(IO) + (add ? 2 : 1) * sizeof(RES)));
-    bulk_load(dst, static_cast<const RES*>(p.s) + row * p.D, n * (unsigned)sizeof(RES), &s_full[stage]);
-    bulk_load(dst + sbytes, static_cast<const IO*>(p.dy) + row * p.D, n * (unsigned)sizeof(IO), &s_full[stage]);
-    if (add) bulk_load(dst + sbytes + ybytes, static_cast<const RES*>(p.dresidual_out) + row * p.D, n * (unsigned)sizeof(RES), &s_full[stage]);
+    expect(&s_full[stage], bytes);
+    bulk_load(dst, static_cast<const RES*>(p.s) + row * p.D, sbytes, &s_full[stage]);
+    bulk_load(dst + sbytes, static_cast<const IO*>(p.dy) + row * p.D, ybytes, &s_full[stage]);
+    if (add) bulk_load(dst + sbytes + ybytes, static_cast<const RES*>(p.dresidual_out) + row * p.D, sbytes, &s_full[stage]);
   };
   if (threadIdx.x == 0)
     for (int i = 0; i < stages - 1; ++i) fill(blockIdx.x + (int64_t)i * gridDim.x, i);
-  using F = Val<VE>;
-  constexpr int M = kVals<VE>;
   F dw[NV][M], db[BIAS ? NV : 1][M];
 #pragma unroll
   for (int k = 0; k < NV; ++k)
@@ -464,93 +459,80 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
   int stage = 0, turn = 0;
   unsigned phase = 0;
   const float over = 1.f / (float)p.D;
-  float mn = 0.f, rn = 0.f;
-  auto stats = [&](int64_t row) {
-    if (row < p.rows) {
-      mn = p.stats[2 * row];
-      rn = p.stats[2 * row + 1];
-    }
-  };
-  stats((int64_t)blockIdx.x * rows + g);
-  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
-    const int64_t here = tile * rows + g;
-    const bool live = here < p.rows;
+  float mn = p.stats[2 * (int64_t)blockIdx.x], rn = p.stats[2 * (int64_t)blockIdx.x + 1];
+  for (int64_t here = blockIdx.x; here < p.rows; here += gridDim.x, turn ^= 1) {
     const float m = mn, r = rn;
-    stats(here + (int64_t)gridDim.x * rows);
+    if (here + gridDim.x < p.rows) {
+      mn = p.stats[2 * (here + gridDim.x)];
+      rn = p.stats[2 * (here + gridDim.x) + 1];
+    }
     const char* at = s_ring + stage * bytes;
-    const RES* bs = reinterpret_cast<const RES*>(at) + g * p.D;
-    const IO* by = reinterpret_cast<const IO*>(at + sbytes) + g * p.D;
-    const RES* ba = reinterpret_cast<const RES*>(at + sbytes + ybytes) + g * p.D;
+    const RES* bs = reinterpret_cast<const RES*>(at);
+    const IO* by = reinterpret_cast<const IO*>(at + sbytes);
+    const RES* ba = reinterpret_cast<const RES*>(at + sbytes + ybytes);
     const bool there = wait_full(&s_full[stage], phase);
     const F off = vset<F>(-m);
     F acc0 = vset<F>(there ? 0.f : NAN), acc1 = acc0;
-    if (live) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = (k * group + j) * VE;
-        if (FULL || c < p.D) {
-          Row<float, VE> w;
-          Row<RES, VE> s;
-          Row<IO, VE> y;
-          F wv[M], sv[M], yv[M];
-          w.load(p.weight, c);
-          w.get(wv);
-          s.load_shared(bs, c);
-          s.get(sv);
-          y.load_shared(by, c);
-          y.get(yv);
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * group + j) * VE;
+      if (FULL || c < p.D) {
+        Row<float, VE> w;
+        Row<RES, VE> s;
+        Row<IO, VE> y;
+        F wv[M], sv[M], yv[M];
+        w.load(p.weight, c);
+        w.get(wv);
+        s.load_shared(bs, c);
+        s.get(sv);
+        y.load_shared(by, c);
+        y.get(yv);
 #pragma unroll
-          for (int i = 0; i < M; ++i) {
-            const F q = vmul(yv[i], wv[i]), xh = vmul(vadd(sv[i], off), vset<F>(r));
-            acc0 = vadd(acc0, q);
-            acc1 = vfma(q, xh, acc1);
-            dw[k][i] = vfma(yv[i], xh, dw[k][i]);
-            if constexpr (BIAS) db[k][i] = vadd(db[k][i], yv[i]);
-          }
+        for (int i = 0; i < M; ++i) {
+          const F q = vmul(yv[i], wv[i]), xh = vmul(vadd(sv[i], off), vset<F>(r));
+          acc0 = vadd(acc0, q);
+          acc1 = vfma(q, xh, acc1);
+          dw[k][i] = vfma(yv[i], xh, dw[k][i]);
+          if constexpr (BIAS) db[k][i] = vadd(db[k][i], yv[i]);
         }
       }
     }
-    if (group <= 32) __syncthreads();                      // (otherwise group_sum has one)
     float sum[2] = {total(acc0), total(acc1)};
     group_sum(sum, group, s_sum, turn);
-    // every thread is past the tile before this one
-    if (threadIdx.x == 0) fill(tile + (int64_t)(stages - 1) * gridDim.x, stage == 0 ? stages - 1 : stage - 1);
+    // every thread is past the row before this one: its place is free
+    if (threadIdx.x == 0) fill(here + (int64_t)(stages - 1) * gridDim.x, stage == 0 ? stages - 1 : stage - 1);
     const float c1 = p.rms ? (there ? 0.f : NAN) : sum[0] * over, c2 = sum[1] * over;
-    if (live) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = (k * group + j) * VE;
-        if (FULL || c < p.D) {
-          Row<float, VE> w;
-          Row<RES, VE> s;
-          Row<IO, VE> y;
-          F wv[M], sv[M], yv[M];
-          w.load(p.weight, c);
-          w.get(wv);
-          s.load_shared(bs, c);
-          s.get(sv);
-          y.load_shared(by, c);
-          y.get(yv);
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * group + j) * VE;
+      if (FULL || c < p.D) {
+        Row<float, VE> w;
+        Row<RES, VE> s;
+        Row<IO, VE> y;
+        F wv[M], sv[M], yv[M];
+        w.load(p.weight, c);
+        w.get(wv);
+        s.load_shared(bs, c);
+        s.get(sv);
+        y.load_shared(by, c);
+        y.get(yv);
 #pragma unroll
-          for (int i = 0; i < M; ++i) {
-            const F xh = vmul(vadd(sv[i], off), vset<F>(r));
-            sv[i] = vfma(vmul(yv[i], wv[i]), vset<F>(r), vfma(xh, vset<F>(-r * c2), vset<F>(-r * c1)));
-          }
-          if (add) {
-            F av[M];
-            s.load_shared(ba, c);
-            s.get(av);
+        for (int i = 0; i < M; ++i) {
+          const F xh = vmul(vadd(sv[i], off), vset<F>(r));
+          sv[i] = vfma(vmul(yv[i], wv[i]), vset<F>(r), vfma(xh, vset<F>(-r * c2), vset<F>(-r * c1)));
+        }
+        if (add) {
+          F av[M];
+          s.load_shared(ba, c);
+          s.get(av);
 #pragma unroll
-            for (int i = 0; i < M; ++i) sv[i] = vadd(sv[i], av[i]);
-          }
-          Row<IO, VE> dx;
-          dx.set(sv);
-          dx.store(p.dx, here * p.D + c);
-          if (p.dresidual != nullptr) {
-            Row<RES, VE> dr;
-            dr.set(sv);
-            dr.store(p.dresidual, here * p.D + c);
-          }
+          for (int i = 0; i < M; ++i) sv[i] = vadd(sv[i], av[i]);
+        }
+        y.set(sv);
+        y.store(p.dx, here * p.D + c);
+        if (p.dresidual != nullptr) {
+          s.set(sv);
+          s.store(p.dresidual, here * p.D + c);
         }
       }
     }
@@ -559,8 +541,8 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
       phase ^= 1;
     }
   }
-  block_parts<VE, NV>(p.dw_part + (size_t)blockIdx.x * p.D, dw, p.D, group, reinterpret_cast<float*>(s_ring));
-  if constexpr (BIAS) block_parts<VE, NV>(p.db_part + (size_t)blockIdx.x * p.D, db, p.D, group, reinterpret_cast<float*>(s_ring));
+  block_parts<VE, NV>(p.dw_part + (size_t)blockIdx.x * p.D, dw, p.D, group, nullptr);
+  if constexpr (BIAS) block_parts<VE, NV>(p.db_part + (size_t)blockIdx.x * p.D, db, p.D, group, nullptr);
 }
 
 // dweight and dbias from the blocks' parts, in a fixed order: 32 columns a block, its slices of threads take every kSlices-th part
@@ -741,15 +723,6 @@ Spread ring_spread(int D, int VE) {
 bool even(const NormParams& p, int VE, int NV) { return p.D == NV * p.group * VE; }
 int block_threads(int group) { return group > 32 ? group : 128; }
 
-// Tiles of a ring of one block: at least two, and for as many blocks of an SM (eight at most) as then fit.  0: it does not fit.
-constexpr int kSharedBytes = 224 << 10;
-int ring_stages(size_t bytes) {
-  for (int blocks = 8; blocks >= 1; --blocks)
-    for (int n = kMostStages; n >= 2; --n)
-      if (blocks * (n * bytes + 2048) <= kSharedBytes) return n;
-  return 0;
-}
-
 template <typename IO, typename RES, int VE, int NV>
 cudaError_t launch_fwd_rows(const NormParams& p, cudaStream_t s) {
   const int threads = block_threads(p.group), rows = threads / p.group;
@@ -775,24 +748,30 @@ cudaError_t launch_fwd_ve(NormParams p, cudaStream_t s) {
   }
 }
 
+// Rows of a block's ring: two at least, and more where the most blocks of an SM (eight) that have two leave room for them.
+constexpr int kSharedBytes = 224 << 10;
+int ring_stages(size_t bytes) {
+  for (int blocks = 8; blocks >= 1; --blocks)
+    for (int n = kMostStages; n >= 2; --n)
+      if (blocks * (n * bytes + 2048) <= kSharedBytes) return n;
+  return 0;
+}
+static_assert(2 * 4 * 256 * 8 * (4 + 2 + 4) + 2048 <= kSharedBytes && 2 * 4 * 256 * 4 * (4 + 4 + 4) + 2048 <= kSharedBytes,
+              "two of the longest rows that ring_spread allows fit");
+
 template <typename IO, typename RES, int VE, int NV, bool BIAS>
-cudaError_t launch_bwd_ring(const NormParams& p, int* parts, bool* done, cudaStream_t s) {
+cudaError_t launch_bwd_ring(const NormParams& p, int* parts, cudaStream_t s) {
   const auto kernel = even(p, VE, NV) ? ssm_norm_ring_bwd_kernel<IO, RES, VE, NV, BIAS, true> : ssm_norm_ring_bwd_kernel<IO, RES, VE, NV, BIAS, false>;
-  const int threads = block_threads(p.group), rows = threads / p.group;
-  const size_t bytes = (size_t)rows * p.D * (sizeof(IO) + (p.dresidual_out != nullptr ? 2 : 1) * sizeof(RES));
+  const size_t bytes = (size_t)p.D * (sizeof(IO) + (p.dresidual_out != nullptr ? 2 : 1) * sizeof(RES));
   const int stages = ring_stages(bytes);
-  *done = stages > 0;
-  if (!*done) return cudaSuccess;
-  const size_t smem = stages * bytes > rows * p.D * sizeof(float) ? stages * bytes : rows * p.D * sizeof(float);
   KernelLimits lim;
-  const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), threads, smem, &lim);
+  const cudaError_t e = kernel_limits(reinterpret_cast<const void*>(kernel), p.group, stages * bytes, &lim);
   if (e != cudaSuccess) return e;
-  const long long tiles = (p.rows + rows - 1) / rows, most = (long long)lim.sms * lim.per_sm;
-  const long long blocks = tiles < most ? tiles : most;
+  const long long most = (long long)lim.sms * lim.per_sm, blocks = p.rows < most ? p.rows : most;
   *parts = (int)(blocks < kMaxParts ? blocks : kMaxParts);
   NormParams q = p;
   if constexpr (BIAS) q.db_part = q.dw_part + (size_t)*parts * p.D;
-  return launch_dependent(kernel, (unsigned)*parts, threads, smem, 1, s, q, stages);
+  return launch_dependent(kernel, (unsigned)*parts, p.group, stages * bytes, 1, s, q, stages);
 }
 
 template <typename IO, typename RES, int VE, int NV, bool BIAS>
@@ -813,38 +792,31 @@ cudaError_t launch_bwd_rows(const NormParams& p, int* parts, cudaStream_t s) {
   return launch_dependent(kernel, (unsigned)blocks, threads, smem, 1, s, q);
 }
 template <typename IO, typename RES, int VE, int NV>
-cudaError_t launch_bwd_nv(const NormParams& p, bool bias, bool ring, int* parts, bool* done, cudaStream_t s) {
-  if constexpr (VE > 2) {
-    if (ring) return bias ? launch_bwd_ring<IO, RES, VE, NV, true>(p, parts, done, s) : launch_bwd_ring<IO, RES, VE, NV, false>(p, parts, done, s);
+cudaError_t launch_bwd_nv(const NormParams& p, bool bias, bool ring, int* parts, cudaStream_t s) {
+  if constexpr (VE > 2 && NV <= 4) {
+    if (ring) return bias ? launch_bwd_ring<IO, RES, VE, NV, true>(p, parts, s) : launch_bwd_ring<IO, RES, VE, NV, false>(p, parts, s);
   }
-  *done = true;
-  return bias ? launch_bwd_rows<IO, RES, VE, NV, true>(p, parts, s) : launch_bwd_rows<IO, RES, VE, NV, false>(p, parts, s);
+  if constexpr (VE <= 2 || NV <= 2)
+    return bias ? launch_bwd_rows<IO, RES, VE, NV, true>(p, parts, s) : launch_bwd_rows<IO, RES, VE, NV, false>(p, parts, s);
+  return cudaErrorInvalidValue;
 }
 
 // Up to 192 threads of two vectors a row's next one waits in registers; where a row is longer the sums take so many that the ring
 // is faster (layer norm with bias, 8192 rows of bf16: 5120 columns 66 us against 97, 4096 64 against 74, 2560 45 against 40).
 template <typename IO, typename RES, int VE>
 cudaError_t launch_bwd_ve(NormParams p, bool bias, int* parts, cudaStream_t s) {
-  bool ring = VE > 2 && p.D > 2 * 192 * VE;
-  Spread sp = ring ? ring_spread(p.D, VE) : spread(p.D, VE, VE <= 2 ? 8 : 2, bwd_threads);
-  for (;;) {
-    p.group = sp.group;
-    bool done = false;
-    cudaError_t e = cudaSuccess;
-    switch (sp.nv) {
-      case 1: e = launch_bwd_nv<IO, RES, VE, 1>(p, bias, ring, parts, &done, s); break;
-      case 2: e = launch_bwd_nv<IO, RES, VE, 2>(p, bias, ring, parts, &done, s); break;
-      case 3: e = launch_bwd_nv<IO, RES, VE, 3>(p, bias, ring, parts, &done, s); break;
-      case 4: e = launch_bwd_nv<IO, RES, VE, 4>(p, bias, ring, parts, &done, s); break;
-      case 8:
-        if constexpr (VE <= 2) e = launch_bwd_nv<IO, RES, VE, 8>(p, bias, ring, parts, &done, s);
-        break;
-      default: break;
-    }
-    if (done || e != cudaSuccess) return e;
-    if (!ring) break;
-    ring = false;                                          // (does not fit the ring)
-    sp = spread(p.D, VE, 4, bwd_threads);
+  const bool ring = VE > 2 && p.D > 2 * 192 * VE;
+  const Spread sp = ring ? ring_spread(p.D, VE) : spread(p.D, VE, VE <= 2 ? 8 : 2, bwd_threads);
+  p.group = sp.group;
+  switch (sp.nv) {
+    case 1: return launch_bwd_nv<IO, RES, VE, 1>(p, bias, ring, parts, s);
+    case 2: return launch_bwd_nv<IO, RES, VE, 2>(p, bias, ring, parts, s);
+    case 3: return launch_bwd_nv<IO, RES, VE, 3>(p, bias, ring, parts, s);
+    case 4: return launch_bwd_nv<IO, RES, VE, 4>(p, bias, ring, parts, s);
+    case 8:
+      if constexpr (VE <= 2) return launch_bwd_nv<IO, RES, VE, 8>(p, bias, false, parts, s);
+      break;
+    default: break;
   }
   *parts = (int)(p.rows < kMaxParts ? p.rows : kMaxParts);
   p.rows_per_part = (int)((p.rows + *parts - 1) / *parts);

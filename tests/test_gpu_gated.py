@@ -87,6 +87,14 @@ def test_forward_backward(batch, L, D, io, decay):
 
 
 @pytest.mark.parametrize("decay", [False, True])
+@pytest.mark.parametrize("batch,L,D,io,reset", [(4, 260, 5120, "bf16", None), (8, 515, 1600, "bf16", 0.01), (2, 1100, 1536, "f32", 0.01),
+                                                (1, 3000, 2560, "bf16", None)])
+def test_layer_widths(batch, L, D, io, reset, decay):
+    # (clusters of other sizes than the shapes above, several rounds each)
+    check(make(batch, L, D, io, decay, seed=L, reset=reset), io)
+
+
+@pytest.mark.parametrize("decay", [False, True])
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("batch,L,D,reset", [(2, 300, 64, 0.02), (1, 77, 33, 0.5), (2, 40, 64, 1.0), (3, 1, 64, 1.0), (1, 4100, 48, 0.003)])
 def test_packed_sequences(batch, L, D, reset, io, decay):

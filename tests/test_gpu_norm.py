@@ -68,7 +68,9 @@ def check(case, io, res, rms, bias, eps=1e-5, dev=None, down=True):
 
 KINDS = [("bf16", None), ("bf16", "bf16"), ("bf16", "f32"), ("f32", None), ("f32", "f32")]
 SHAPES = [(1, 64), (1, 1), (3, 2), (5, 7), (2, 31), (4, 33), (7, 100), (33, 96), (300, 64), (17, 256), (9, 1001), (5, 1002),
-          (6, 2048), (150, 520), (3, 5120), (2, 8192), (2, 10007), (700, 136), (1500, 24)]
+          (6, 2048), (150, 520), (3, 5120), (2, 8192), (2, 10007), (700, 136), (1500, 24),
+          # more rows than blocks at once, in registers and through the ring; rows of whole pairs; rows of no kernel but the long ones'
+          (1400, 1024), (1300, 4096), (900, 1802), (5, 5002), (2, 17000)]
 
 
 @pytest.mark.parametrize("rms,bias", [(False, True), (True, False), (True, True), (False, False)])
