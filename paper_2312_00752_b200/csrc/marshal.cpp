@@ -34,13 +34,17 @@ PyObject* g_out_of_memory = nullptr;   // torch.OutOfMemoryError
   X(ssm_scan_fwd_state) X(ssm_scan_fwd_fused_dt) X(ssm_scan_fwd_static) X(ssm_scan_bwd) X(ssm_scan_bwd_state)     \
   X(ssm_scan_bwd_fused_dt) X(ssm_scan_bwd_fused_dt_state) X(ssm_step) X(ssm_scan_fwd_workspace_bytes)             \
   X(ssm_scan_bwd_workspace_bytes) X(ssm_scan_saved_state_bytes) X(ssm_status_string) X(ssm_conv1d_fwd)            \
-  X(ssm_conv1d_bwd) X(ssm_conv1d_bwd_workspace_bytes) X(ssm_gated_saved_state_bytes) X(ssm_gated_fwd)             \
-  X(ssm_gated_bwd_workspace_bytes) X(ssm_gated_bwd) X(ssm_gated_step) X(ssm_norm_fwd)                             \
-  X(ssm_norm_bwd_workspace_bytes) X(ssm_norm_bwd)
+  X(ssm_conv1d_bwd) X(ssm_conv1d_bwd_workspace_bytes)
+// those of the block around the scan, which a library may be without (a call then raises)
+#define SSM_BLOCK_ENTRY_POINTS(X)                                                                                 \
+  X(ssm_gated_saved_state_bytes) X(ssm_gated_fwd) X(ssm_gated_bwd_workspace_bytes) X(ssm_gated_bwd)               \
+  X(ssm_gated_step) X(ssm_norm_fwd) X(ssm_norm_bwd_workspace_bytes) X(ssm_norm_bwd)
 struct Api {
 #define X(name) decltype(&::name) name;
   SSM_ENTRY_POINTS(X)
+  SSM_BLOCK_ENTRY_POINTS(X)
 #undef X
+  bool block;   // the latter are there
 } api;
 
 struct Raised {};   // a Python exception is set
@@ -502,6 +506,7 @@ PyObject* conv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---------------------------------------------------------------------------- gated linear recurrence, norm
 const at::Tensor& first(PyObject* o, const char* name) {
+  if (!api.block) raise("the library has no gated recurrence and norm");
   const at::Tensor* t = tensor(o, name);
   if (t == nullptr || !t->is_cuda()) raise(std::string(name) + " must be a CUDA tensor");
   return *t;
@@ -859,6 +864,12 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   api.name = reinterpret_cast<decltype(api.name)>(dlsym(lib, #name));                  \
   if (api.name == nullptr) return PyErr_Format(PyExc_OSError, "%s: no symbol " #name, path);
   SSM_ENTRY_POINTS(X)
+#undef X
+  api.block = true;
+#define X(name)                                                                        \
+  api.name = reinterpret_cast<decltype(api.name)>(dlsym(lib, #name));                  \
+  api.block = api.block && api.name != nullptr;
+  SSM_BLOCK_ENTRY_POINTS(X)
 #undef X
   Py_INCREF(a[1]);
   Py_XDECREF(g_error);
