@@ -117,14 +117,20 @@ void* stream_of(PyObject* stream, const at::Tensor& x) {
   return s;
 }
 
-// A new result of a call on `stream`.  It is a block of the current stream; where that is another one the allocator is told, so
-// that a result that is dropped early is not given to other tensors while the call still writes to it.
+// A new result of a call on `stream`.  Where that is not the current one it is a block of that stream's own, like the scratch: one of
+// the current stream's may have been given back by work there that is still under way, which the call does not wait for.  The
+// allocator is told that the current stream uses it too, so that a result that is dropped is not given to other tensors before.
 at::Tensor result(at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& like, void* stream) {
-  at::Tensor t = empty(shape, dtype, like);
-  const auto s = static_cast<cudaStream_t>(stream);
   const c10::DeviceIndex dev = like.device().index();
-  if (c10::cuda::getCurrentCUDAStream(dev).stream() != s)
-    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), c10::cuda::getStreamFromExternal(s, dev));
+  if (!like.is_cuda()) raise("x must be a CUDA tensor");
+  const auto current = c10::cuda::getCurrentCUDAStream(dev);
+  if (current.stream() == static_cast<cudaStream_t>(stream)) return empty(shape, dtype, like);
+  at::Tensor t;
+  {
+    const c10::cuda::CUDAStreamGuard on(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), dev));
+    t = empty(shape, dtype, like);
+  }
+  c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
   return t;
 }
 

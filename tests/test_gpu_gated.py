@@ -395,3 +395,24 @@ def test_against_differences_of_the_call_itself():
         want = float((g["d" + name].double() * way).sum())
         # differences of sums of a few hundred terms of size 1, each good to 1e-6, over 2^-9; and eps^2 of the third derivative
         assert abs(num - want) <= 2e-2 + 1e-3 * abs(want), (name, num, want)
+
+
+def test_results_of_a_call_on_another_stream_are_no_memory_that_the_current_one_still_writes():
+    import torch
+    from paper_2312_00752_b200 import binding as K
+    x, gate, w = torch.randn(4, 1000, 64, device="cuda"), torch.randn(4, 1000, 64, device="cuda"), torch.ones(64, device="cuda")
+    s = torch.cuda.Stream()
+    run = lambda **kw: (K.ssm_gated_fwd(x, gate, **kw), K.ssm_norm_fwd(x, w, **kw))
+    ref = run()
+    run(stream=s)
+    torch.cuda.synchronize()
+    late = [torch.empty_like(x) for _ in range(8)]
+    torch.cuda._sleep(200_000_000)                # the writes below wait behind this, a tenth of a second
+    for v in late:
+        v.fill_(7.0)
+    v = late = None                               # (their memory is free again for the current stream, in its order)
+    got = run(stream=s)
+    s.synchronize()
+    assert not torch.cuda.current_stream().query()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(ref, got))
