@@ -129,6 +129,11 @@ struct Row {   // VE elements of type T as they lie in memory
   }
 };
 
+// the thread within its group, the group within the block, groups of a block
+__device__ __forceinline__ int lane_of(int group) { return group > 32 ? threadIdx.x : threadIdx.x & (group - 1); }
+__device__ __forceinline__ int group_index(int group) { return group > 32 ? 0 : threadIdx.x >> (31 - __clz(group)); }
+__device__ __forceinline__ int groups_of(int group) { return group > 32 ? 1 : blockDim.x >> (31 - __clz(group)); }
+
 constexpr int kMaxWarps = 32;
 // threads of a block, by vectors a thread: what the registers allow
 constexpr int fwd_threads(int VE, int NV) { return VE * NV > 48 ? 384 : VE * NV > 16 ? 512 : 1024; }
@@ -157,15 +162,18 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*s_su
   }
 }
 
-template <typename IO, typename RES, int VE, int NV>
+// MODE: 1 a residual is added, 2 there is a bias, 4 look at the pointers (the tests, and the residual's rounding where there is none,
+// were a tenth of the instructions of a row)
+template <typename IO, typename RES, int VE, int NV, int MODE>
 __global__ void __launch_bounds__(fwd_threads(VE, NV)) ssm_norm_rows_fwd_kernel(const NormParams p) {
   __shared__ float s_sum[2][kMaxWarps][1];
-  const int group = p.group, j = threadIdx.x % group;
-  const int64_t here = (int64_t)blockIdx.x * (blockDim.x / group) + threadIdx.x / group;
+  const int group = p.group, j = lane_of(group);
+  const int64_t here = (int64_t)blockIdx.x * groups_of(group) + group_index(group);
   const bool live = here < p.rows;
   const int64_t at0 = (live ? here : 0) * p.D;          // (groups past the last row run along on the first)
   dependency_wait();
-  const bool add = p.residual != nullptr;
+  const bool add = MODE & 4 ? p.residual != nullptr : MODE & 1, bias = MODE & 4 ? p.bias != nullptr : (MODE & 2) != 0;
+  const bool keep = add && p.residual_out != nullptr && live;
   Row<IO, VE> x[NV];
   Row<RES, VE> s[NV];
 #pragma unroll
@@ -191,10 +199,10 @@ __global__ void __launch_bounds__(fwd_threads(VE, NV)) ssm_norm_rows_fwd_kernel(
         for (int i = 0; i < M; ++i) v[i] = vadd(v[i], a[i]);
       }
       s[k].set(v);
-      s[k].get(v);
+      if (add) s[k].get(v);
 #pragma unroll
       for (int i = 0; i < M; ++i) acc = vadd(acc, v[i]);
-      if (p.residual_out != nullptr && live) s[k].store(p.residual_out, at0 + c);
+      if (keep) s[k].store(p.residual_out, at0 + c);
     }
   }
   const float over = 1.f / (float)p.D;
@@ -229,14 +237,14 @@ __global__ void __launch_bounds__(fwd_threads(VE, NV)) ssm_norm_rows_fwd_kernel(
       s[k].get(v);
       w.load(p.weight, c);
       w.get(wv);
-      if (p.bias != nullptr) {
+      if (bias) {
         b.load(p.bias, c);
         b.get(bv);
       }
 #pragma unroll
       for (int i = 0; i < M; ++i) {
         const F xh = vmul(vadd(v[i], off), vset<F>(r));
-        v[i] = p.bias != nullptr ? vfma(xh, wv[i], bv[i]) : vmul(xh, wv[i]);
+        v[i] = bias ? vfma(xh, wv[i], bv[i]) : vmul(xh, wv[i]);
       }
       y.set(v);
       y.store(p.y, at0 + c);
@@ -251,9 +259,9 @@ __global__ void __launch_bounds__(fwd_threads(VE, NV)) ssm_norm_rows_fwd_kernel(
 // the sum of a block's groups' column sums v, in order; s_part: [groups][D] where there is more than one
 template <int VE, int NV>
 __device__ __forceinline__ void block_parts(float* __restrict__ out, const Val<VE> (&v)[NV][kVals<VE>], int D, int group, float* s_part) {
-  const int j = threadIdx.x % group, groups = blockDim.x / group;
+  const int j = lane_of(group), groups = groups_of(group);
   if (groups > 1) __syncthreads();
-  float* to = groups > 1 ? s_part + threadIdx.x / group * D : out;
+  float* to = groups > 1 ? s_part + group_index(group) * D : out;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * group + j) * VE;
@@ -277,11 +285,12 @@ template <typename IO, typename RES, int VE, int NV, bool BIAS, bool FULL>
 __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(const NormParams p) {
   __shared__ float s_sum[2][kMaxWarps][2];
   extern __shared__ float s_part[];                      // groups of 32 threads or fewer: [groups][D]
-  const int group = p.group, j = threadIdx.x % group;
-  const int groups = blockDim.x / group;
+  const int group = p.group, j = lane_of(group);
+  const int groups = groups_of(group);
   const int64_t apart = (int64_t)gridDim.x * groups;
   const int64_t first = (int64_t)blockIdx.x * groups;    // (the block's groups run the same number of turns)
-  int64_t here = first + threadIdx.x / group;
+  int64_t here = first + group_index(group);
+  const bool arrives = p.dresidual_out != nullptr, both = p.dresidual != nullptr;
   dependency_wait();
   using F = Val<VE>;
   constexpr int M = kVals<VE>;
@@ -323,7 +332,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
     m = mn;
     r = rn;
     Row<RES, VE> add[NV];
-    if (p.dresidual_out != nullptr && live) {
+    if (arrives && live) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * group + j) * VE;
@@ -374,7 +383,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
             const F xh = vmul(vadd(sv[i], off), vset<F>(r));
             sv[i] = vfma(vmul(yv[i], wv[i]), vset<F>(r), vfma(xh, vset<F>(-r * c2), vset<F>(-r * c1)));
           }
-          if (p.dresidual_out != nullptr) {
+          if (arrives) {
             F av[M];
             add[k].get(av);
 #pragma unroll
@@ -383,7 +392,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_rows_bwd_kernel(
           Row<IO, VE> dx;
           dx.set(sv);
           dx.store(p.dx, here * p.D + c);
-          if (p.dresidual != nullptr) {
+          if (both) {
             Row<RES, VE> dr;
             dr.set(sv);
             dr.store(p.dresidual, here * p.D + c);
@@ -432,7 +441,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
   __shared__ uint64_t s_full[kMostStages];
   extern __shared__ __align__(128) char s_ring[];
   const int group = p.group, j = threadIdx.x;
-  const bool add = p.dresidual_out != nullptr;
+  const bool add = p.dresidual_out != nullptr, both = p.dresidual != nullptr;
   const int sbytes = p.D * (int)sizeof(RES), ybytes = p.D * (int)sizeof(IO), bytes = sbytes + ybytes + (add ? sbytes : 0);
   if (threadIdx.x == 0)
     for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&s_full[i])) : "memory");
@@ -530,7 +539,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
         }
         y.set(sv);
         y.store(p.dx, here * p.D + c);
-        if (p.dresidual != nullptr) {
+        if (both) {
           s.set(sv);
           s.store(p.dresidual, here * p.D + c);
         }
@@ -727,7 +736,16 @@ template <typename IO, typename RES, int VE, int NV>
 cudaError_t launch_fwd_rows(const NormParams& p, cudaStream_t s) {
   const int threads = block_threads(p.group), rows = threads / p.group;
   const unsigned blocks = (unsigned)((p.rows + rows - 1) / rows);
-  return launch_dependent(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV>, blocks, threads, 0, 1, s, p);
+  auto launch = [&](auto kernel) { return launch_dependent(kernel, blocks, threads, 0, 1, s, p); };
+  if constexpr (VE > 2) {
+    if (p.residual != nullptr)
+      return p.bias != nullptr ? launch(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV, 3>) : launch(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV, 1>);
+    if constexpr (std::is_same<IO, RES>::value)
+      return p.bias != nullptr ? launch(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV, 2>) : launch(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV, 0>);
+    return cudaErrorInvalidValue;                          // (a residual's type is that of x without one)
+  } else {
+    return launch(ssm_norm_rows_fwd_kernel<IO, RES, VE, NV, 4>);
+  }
 }
 
 template <typename IO, typename RES, int VE>
