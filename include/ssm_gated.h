@@ -32,7 +32,8 @@
  *     form: the factors 1 - sigma of dgate and din_gate carry an absolute error of 2^-25, so that a gate that is saturated beyond
  *     17 gets the gradient 0.)
  *   - Every pointer is aligned to its element.  Rows that begin and end on 16 bytes take the widest copies, such on 4 bytes
- *     narrower ones; the latter are half as fast, odd rows of bf16 a third.
+ *     narrower ones, others single elements, each slower than the one before.  bf16 pairs of channels also want A, h0, h_last,
+ *     dh_last, dh0 and the saved states aligned to 8 bytes; otherwise single elements move.
  *   - Results are bitwise reproducible for the same problem, pointers' alignment and presence of optional arguments.
  *   - NaN and Inf propagate along the recurrence (and not across a reset).  A > 0 is not validated and gives NaN.
  */

@@ -17,7 +17,8 @@
  * pointers' alignment (fixed summation orders, no atomics).  Layouts: x, y, dy, dx dense [rows][D] io_dtype; residual,
  * residual_out, dresidual_out, dresidual dense [rows][D] residual_dtype; s is residual_out, or x where there is no residual;
  * weight, bias, dweight, dbias float32 [D]; stats float32 [rows][2] (m, r).  Arithmetic and sums are float32.  Every
- * pointer is aligned to its element; rows of whole 16 bytes at 16-byte aligned pointers take wide accesses.
+ * pointer is aligned to its element; rows of whole 16 bytes at aligned pointers (to 16 bytes, float32 ones beside bf16 io to 32)
+ * take wide accesses, bf16 rows of whole pairs (4 and 8 bytes) narrower ones.
  * NaN and Inf propagate within their row (and into dweight and dbias).
  */
 #ifndef SSM_NORM_H_

@@ -10,6 +10,11 @@
 // Decay form, with w = beta iota and inv = 1 / beta kept: iota = w inv, u / (1 - a^2) = iota inv x, so that
 //     dx = mu w,  din_gate = dx x (1 - iota),  m = mu a (h[t-1] - a iota inv x),  dgate = m rho A (1 - rho),  dA = sum m rho
 // take no special-function operation beyond the five of the gates.
+//
+// What bounds it: 10 or 14 bytes an element and the saved states, about 120 instructions for a pair of channels in the decay form,
+// and the registers of what waits for the adjoint: ten values a step and pair, 164 in all, three blocks an SM ((8, 2048, 2560) bf16
+// 154 us, 58 % of the copy bandwidth; four blocks of 128 registers 226, two 200).  The convex form keeps six and runs four
+// blocks ((4, 2048, 5120) bf16 97 us, 66 %).
 #include <cmath>
 #include <type_traits>
 

@@ -1,12 +1,16 @@
 // Forward kernel of the gated linear recurrence (include/ssm_gated.h).
 //
 // What a step does to a state is affine, h -> a h + u, and so is what a run of steps does: h -> P h + S.  A block owns 32
-// lanes of channels (one or two each) and walks the sequence in tiles; in a tile every one of its warps takes kGatedSteps
+// lanes of channels (one or two each) and walks the sequence in tiles; in a tile every one of its warps takes 16
 // adjacent steps, forms their a and u once, in registers, and their (P, S).  The warps' pairs meet in shared memory, each warp
 // folds those before it onto the state that entered the tile, and runs its steps again from there, which is one multiply-add
 // each.  So x and the gates are read once and y written once, and a warp's loads for the next tile are under way while it does.
-// Where the channels alone do not fill the GPU, the blocks of a cluster take adjacent tiles of the same channels and hand
-// their tile's (P, S) to one another through distributed shared memory: one cluster barrier a round, nothing waits on memory.
+// Where the channels alone do not fill the GPU evenly, the blocks of a cluster take adjacent tiles of the same channels and
+// send their tile's (P, S) into one another's shared memory, once a round.
+//
+// What bounds it: 6 (convex) or 8 (decay) bytes an element, 2 or 4 special-function operations and about 43 or 59 instructions for a
+// pair of channels.  (4, 2048, 5120) bf16: convex 52 us, 74 % of the copy bandwidth, lost in the balance of its blocks ((4, 2048,
+// 9472), whose groups of channels fill the GPU exactly, 91 %); decay 76 us, 68 %, FP32 pipe and issue.
 //
 // P may underflow although no retention is zero, and zero times an infinite state would be NaN where the steps one by one
 // keep it infinite: it is held at the least normal number, 2^-126 of the state at most, far below its rounding.  A step that
@@ -20,8 +24,8 @@ namespace ssm {
 
 namespace {
 
-constexpr int S = 16;                // steps of a warp in a tile
-constexpr int W = 4;                 // warps of a block
+constexpr int S = 16;                // steps of a warp in a tile (8, with more warps an SM: decay 80 us against 76)
+constexpr int W = 4;                 // warps of a block (8: 86)
 constexpr int kTile = S * W;         // steps of a tile
 
 // The inputs of a warp's steps on their way from global memory, a tile ahead: two buffers of half the steps each, of the warp's own
