@@ -407,7 +407,7 @@ def test_results_of_a_call_on_another_stream_are_no_memory_that_the_current_one_
     run(stream=s)
     torch.cuda.synchronize()
     late = [torch.empty_like(x) for _ in range(8)]
-    torch.cuda._sleep(200_000_000)                # the writes below wait behind this, a tenth of a second
+    torch.cuda._sleep(400_000_000)                # the writes below wait behind this, a fifth of a second
     for v in late:
         v.fill_(7.0)
     v = late = None                               # (their memory is free again for the current stream, in its order)
