@@ -288,6 +288,15 @@ __device__ __forceinline__ void cp_async16(void* smem_dst, const void* gmem_src,
   const int bytes = valid ? 16 : 0;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(gmem_src), "r"(bytes) : "memory");
 }
+// Sets up `n` barriers in shared memory for one arrival a phase; one thread calls it, before a barrier of the block (of the
+// cluster, where other blocks signal them).  That orders the set-up among threads only: bulk copies signal through the
+// asynchronous proxy and other blocks' stores from outside the block, and each needs its fence.
+__device__ __forceinline__ void set_up_barriers(uint64_t* barriers, int n) {
+  for (int i = 0; i < n; ++i)
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((unsigned)__cvta_generic_to_shared(barriers + i)) : "memory");
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
 __device__ __forceinline__ int ld_acquire(const int* p) {
   int v;
   asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");

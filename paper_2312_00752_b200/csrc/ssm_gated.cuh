@@ -197,9 +197,6 @@ __device__ __forceinline__ void send(unsigned to, unsigned barrier, const Affine
                "f"(v.S.x), "f"(v.S.y), "r"(barrier)
                : "memory");
 }
-__device__ __forceinline__ void barrier_init(const void* barrier) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(barrier)) : "memory");
-}
 __device__ __forceinline__ void barrier_expect(const void* barrier, unsigned bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
 }

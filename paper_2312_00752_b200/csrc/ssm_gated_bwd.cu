@@ -141,10 +141,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
   int q = p.nck - 1 - (rank * W + w);                // this warp's run of steps in the round: from the end towards 0, then below
   const int step = W * C;
   if (C > 1) {
-    if (threadIdx.x == 0) {
-      barrier_init(&s_there[0]);
-      barrier_init(&s_there[1]);
-    }
+    if (threadIdx.x == 0) set_up_barriers(s_there, 2);
     cluster_sync();
   }
   In in;

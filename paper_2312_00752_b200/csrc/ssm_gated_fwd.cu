@@ -125,10 +125,7 @@ __global__ void __launch_bounds__(32 * W, DECAY && !RESET ? 3 : 4) ssm_gated_fwd
   const int step = kTile * C;                        // from a tile to the next one of this block
   int t0 = (rank * W + w) * S;                       // this warp's first step in the round
   if (C > 1) {
-    if (threadIdx.x == 0) {
-      barrier_init(&s_there[0]);
-      barrier_init(&s_there[1]);
-    }
+    if (threadIdx.x == 0) set_up_barriers(s_there, 2);
     cluster_sync();                                  // (every block is there, its barriers set up)
   }
   In in;

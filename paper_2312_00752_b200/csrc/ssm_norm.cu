@@ -443,8 +443,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
   const int group = p.group, j = threadIdx.x;
   const bool add = p.dresidual_out != nullptr, both = p.dresidual != nullptr;
   const int sbytes = p.D * (int)sizeof(RES), ybytes = p.D * (int)sizeof(IO), bytes = sbytes + ybytes + (add ? sbytes : 0);
-  if (threadIdx.x == 0)
-    for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&s_full[i])) : "memory");
+  if (threadIdx.x == 0) set_up_barriers(s_full, stages);
   __syncthreads();
   dependency_wait();
   auto fill = [&](int64_t row, int stage) {                // thread 0
