@@ -37,8 +37,8 @@ enum {
 };
 
 typedef struct {
-  int64_t rows;            /* >= 1 */
-  int32_t D;               /* >= 1 */
+  int64_t rows;            /* 1 .. 2^31 - 1 */
+  int32_t D;               /* 1 .. 2^28 */
   int32_t io_dtype;        /* ssm_dtype_t */
   int32_t residual_dtype;  /* ssm_dtype_t: io_dtype or SSM_F32; io_dtype where there is no residual */
   uint32_t flags;          /* SSM_NORM_FLAG_* */

@@ -681,7 +681,7 @@ ssm_status_t validate(const ssm_norm_problem_t* p) {
     if (!(p->flags & SSM_NORM_FLAG_HAS_RESIDUAL)) return SSM_ERR_INVALID_ARG;
     if (p->residual_dtype != SSM_F32) return SSM_ERR_UNSUPPORTED;
   }
-  if (p->rows > INT32_MAX) return SSM_ERR_UNSUPPORTED;
+  if (p->rows > INT32_MAX || p->D > 1 << 28) return SSM_ERR_UNSUPPORTED;   // (blocks of a grid; a row's columns, and a step past them, fit 32 bits)
   return SSM_OK;
 }
 
