@@ -115,21 +115,17 @@ def load_library() -> ctypes.CDLL:
     lib.ssm_conv1d_bwd_workspace_bytes.argtypes = [CP]
     lib.ssm_conv1d_bwd.restype = ctypes.c_int
     lib.ssm_conv1d_bwd.argtypes = [CP] + [vp] * 9 + [vp, sz, vp]
+    # the gated recurrence and the norm, which a library may be without (their calls then raise)
     GP, NP = ctypes.POINTER(ssm_gated_problem_t), ctypes.POINTER(ssm_norm_problem_t)
-    for name, problem in (("ssm_gated_saved_state_bytes", GP), ("ssm_gated_bwd_workspace_bytes", GP),
-                          ("ssm_norm_bwd_workspace_bytes", NP)):
-        getattr(lib, name).restype = sz
-        getattr(lib, name).argtypes = [problem]
-    lib.ssm_gated_fwd.restype = ctypes.c_int
-    lib.ssm_gated_fwd.argtypes = [GP] + [vp] * 9 + [vp]
-    lib.ssm_gated_bwd.restype = ctypes.c_int
-    lib.ssm_gated_bwd.argtypes = [GP] + [vp] * 14 + [vp, sz, vp]
-    lib.ssm_gated_step.restype = ctypes.c_int
-    lib.ssm_gated_step.argtypes = [GP] + [vp] * 7 + [vp]
-    lib.ssm_norm_fwd.restype = ctypes.c_int
-    lib.ssm_norm_fwd.argtypes = [NP] + [vp] * 7 + [vp]
-    lib.ssm_norm_bwd.restype = ctypes.c_int
-    lib.ssm_norm_bwd.argtypes = [NP] + [vp] * 9 + [vp, sz, vp]
+    for name, result, arguments in (("ssm_gated_saved_state_bytes", sz, [GP]), ("ssm_gated_fwd", ctypes.c_int, [GP] + [vp] * 9 + [vp]),
+                                    ("ssm_gated_bwd_workspace_bytes", sz, [GP]),
+                                    ("ssm_gated_bwd", ctypes.c_int, [GP] + [vp] * 14 + [vp, sz, vp]),
+                                    ("ssm_gated_step", ctypes.c_int, [GP] + [vp] * 7 + [vp]),
+                                    ("ssm_norm_fwd", ctypes.c_int, [NP] + [vp] * 7 + [vp]), ("ssm_norm_bwd_workspace_bytes", sz, [NP]),
+                                    ("ssm_norm_bwd", ctypes.c_int, [NP] + [vp] * 9 + [vp, sz, vp])):
+        if hasattr(lib, name):
+            getattr(lib, name).restype = result
+            getattr(lib, name).argtypes = arguments
     lib.ssm_scan_bwd_fused_dt_state.restype = ctypes.c_int
     lib.ssm_scan_bwd_fused_dt_state.argtypes = [P] + [vp] * 21 + [vp, sz, vp]
     lib.ssm_scan_bwd_state.restype = ctypes.c_int
