@@ -171,8 +171,9 @@ struct ReduceParams {
   int* clear;             // status word to zero, of a call none of whose kernels reads or raises it; null: none
 };
 
-// SMs of the current device and blocks of a kernel that fit one of them, with `smem` bytes of dynamic shared memory, which
-// the kernel is allowed to use from then on.  Asked of the runtime once per thread, kernel and device (ssm_launch.cu).
+// SMs of the current device and blocks of a kernel of `threads` threads that fit one of them, with `smem` bytes of dynamic shared
+// memory, which the kernel is allowed to use from then on.  Asked of the runtime once per host thread, kernel, sizes and device
+// (ssm_launch.cu).
 struct KernelLimits {
   int sms, per_sm;
 };

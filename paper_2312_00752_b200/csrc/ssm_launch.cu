@@ -10,23 +10,23 @@ namespace {
 struct Key {
   const void* kernel;
   size_t smem;
-  int device;
-  bool operator==(const Key& o) const { return kernel == o.kernel && smem == o.smem && device == o.device; }
+  int threads, device;   // (a kernel may be launched with blocks of several sizes, each with an occupancy of its own)
+  bool operator==(const Key& o) const { return kernel == o.kernel && smem == o.smem && threads == o.threads && device == o.device; }
 };
 struct KeyHash {
   size_t operator()(const Key& k) const {
-    return (reinterpret_cast<size_t>(k.kernel) >> 4) * 31 + k.smem * 17 + (size_t)k.device;
+    return (reinterpret_cast<size_t>(k.kernel) >> 4) * 31 + k.smem * 17 + (size_t)k.threads * 7 + (size_t)k.device;
   }
 };
 }  // namespace
 
 cudaError_t kernel_limits(const void* kernel, int threads, size_t smem, KernelLimits* out) {
-  // one table per thread: no lock, and at most one entry per kernel, shared-memory size and device
+  // one table per thread: no lock, and at most one entry per kernel, block and shared-memory size and device
   thread_local std::unordered_map<Key, KernelLimits, KeyHash> known;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  const Key key{kernel, smem, dev};
+  const Key key{kernel, smem, threads, dev};
   const auto it = known.find(key);
   if (it != known.end()) {
     *out = it->second;
