@@ -28,9 +28,7 @@
  *     written.  y, dy: dense [batch][L][D] io_dtype.
  *   - A, dA float32 [D]; h0, h_last, dh_last, dh0 and the h of ssm_gated_step float32 [batch][D]; reset one byte per step,
  *     [batch][L] (ssm_gated_step: [batch]).
- *   - Arithmetic, states and sums are float32; y and the gradients of the inputs are rounded once to io_dtype.  (bf16 io, decay
- *     form: the factors 1 - sigma of dgate and din_gate carry an absolute error of 2^-25, so that a gate that is saturated beyond
- *     17 gets the gradient 0.)
+ *   - Arithmetic, states and sums are float32; y and the gradients of the inputs are rounded once to io_dtype.
  *   - Every pointer is aligned to its element.  Rows that begin and end on 16 bytes take the widest copies, such on 4 bytes
  *     narrower ones, others single elements, each slower than the one before.  bf16 pairs of channels also want A, h0, h_last,
  *     dh_last, dh0 and the saved states aligned to 8 bytes; otherwise single elements move.

@@ -107,12 +107,19 @@ struct Feed {
   }
 };
 
-// 1 - g of a gate g = sigma(z).  float32 io forms it without cancellation, by another exponential (it has twice the bytes to wait
-// for); for bf16 the difference's absolute error of 2^-25 is below the gradient's rounding up to z = 9, where it is 1e-4.
-template <typename IO, class F>
-__device__ __forceinline__ F rest(F z, F g) {
+// 1 - g of a gate g = sigma(z).  Where g is near 1 the difference cancels: its absolute error is up to 2.5 * 2^-25 (the sum 1 + e, the
+// reciprocal and the difference are rounded), which is 3e-5 of it at z = kOpen, a hundredth of a bf16's rounding, and all of it at 17.
+// e g has no such limit and takes another exponential (exact).  float32 io always forms it so; with bf16 it is 12 % of the kernel's
+// time ((8, 2048, 2560) 174 us, 154 without), so that a warp looks for gates above kOpen among its own first: 156.
+constexpr float kOpen = 6.f;
+template <class F, class Exact>
+__device__ __forceinline__ F rest(F z, F g, Exact exact) {   // exact: bool, or known when compiled
   const F near = vfma(g, vset<F>(-1.f), vset<F>(1.f));
-  if constexpr (sizeof(IO) == 2) return near;
+  if constexpr (std::is_same<Exact, bool>::value) {
+    if (!exact) return near;
+  } else if constexpr (!Exact::value) {
+    return near;
+  }
   const F far = vmul(vmap(vmul(z, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), g);
   return vmap(g, near, far, [](float v, float n, float f) { return v < 0.5f ? n : f; });
 }
@@ -126,6 +133,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
   using No = std::false_type;
   constexpr int V = kWidth<F>;
   constexpr int kAhead = COPY > 0 ? 2 : 1;           // tiles fetched before the first is looked at
+  constexpr bool kLook = DECAY && sizeof(IO) == 2;   // whether a gate is above kOpen is asked
   extern __shared__ __align__(16) char s_feed[];
   __shared__ Affine<F> s_warp[2][W][32];
   __shared__ Affine<F> s_block[2][kGatedCluster][32];
@@ -175,6 +183,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
     // of each step: retention, state before it, and convex: g; decay: rho, w = beta iota, inv = 1 / beta
     F a[S], before[S], g[S], wi[DECAY ? S : 1], inv[DECAY ? S : 1];
     Affine<F> mine{vset<F>(1.f), vset<F>(0.f)};
+    F most = vset<F>(0.f);                           // of the gates
     const unsigned cuts = RESET ? __ballot_sync(~0u, mask0 != 0) : 0u;
     mask0 = mask1;
     mask1 = mask_at(q - 2 * step);
@@ -198,7 +207,9 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
           } else {
             F oa;
             g[k] = vmap(vadd(vmap(vmul(z, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f)), [](float v) { return rcp_approx(v); });
-            const F iota = vmap(vadd(vmap(vmul(in.get(DECAY ? 3 : 0, k, stage), vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f)),
+            const F zi = in.get(DECAY ? 3 : 0, k, stage);
+            if constexpr (kLook) most = vmap(most, z, zi, [](float v, float p, float q) { return fmaxf(v, fmaxf(p, q)); });
+            const F iota = vmap(vadd(vmap(vmul(zi, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), vset<F>(1.f)),
                                 [](float v) { return rcp_approx(v); });
             if constexpr (SMALL) decay_pair_small(vmul(g[k], At), a[k], oa);
             else decay_pair(vmul(g[k], At), a[k], oa);
@@ -270,7 +281,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
       char* const ox = reinterpret_cast<char*>(static_cast<IO*>(p.dx) + row * p.ld_dx + d);
       char* const og = reinterpret_cast<char*>(static_cast<IO*>(p.dgate) + row * p.ld_dgate + d);
       char* const oi = DECAY ? reinterpret_cast<char*>(static_cast<IO*>(p.din_gate) + row * p.ld_din + d) : nullptr;
-      auto gradients = [&](auto all_steps) {
+      auto gradients = [&](auto all_steps, auto exact) {
 #pragma unroll
         for (int k = S - 1; k >= 0; --k) {
           if (decltype(all_steps)::value || k < n) {
@@ -283,10 +294,10 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
             } else {
               const F iota = vmul(wi[k], inv[k]);
               dx = vmul(mu, wi[k]);
-              di = vmul(vmul(dx, x), rest<IO>(in.get(DECAY ? 3 : 0, k, stage), iota));
+              di = vmul(vmul(dx, x), rest(in.get(DECAY ? 3 : 0, k, stage), iota, exact));
               const F m = vmul(vmul(back, vfma(vmul(a[k], vset<F>(-1.f)), vmul(vmul(iota, inv[k]), x), before[k])), g[k]);   // m rho
               dA = vadd(dA, m);
-              dg = vmul(vmul(m, A), rest<IO>(in.get(1, k, stage), g[k]));
+              dg = vmul(vmul(m, A), rest(in.get(1, k, stage), g[k], exact));
             }
             if (live) {
               *reinterpret_cast<Raw*>(ox + (uint64_t)lx * k) = Io::close(dx);
@@ -297,8 +308,20 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
           }
         }
       };
-      if (n >= S) gradients(Yes{});
-      else gradients(No{});
+      if constexpr (kLook) {
+        bool open = false;
+        vmap(most, [&](float v) { open = open || v > kOpen; return v; });
+        open = __any_sync(~0u, open);
+        // Rows of whole 16 bytes take a body for either case (asked step by step 170 us instead of 156); for others, whose copies are
+        // four times as many instructions, two bodies are the longer way ((2, 2048, 1026) 33 us against 31.5).
+        if (n < S) gradients(No{}, open);
+        else if constexpr (COPY != 16) gradients(Yes{}, open);
+        else if (open) gradients(Yes{}, Yes{});
+        else gradients(Yes{}, No{});
+      } else {
+        if (n >= S) gradients(Yes{}, Yes{});
+        else gradients(No{}, Yes{});
+      }
     }
     in.release();
     if constexpr (COPY > 0) in.issue(rows_of(q - 2 * step), half, step * S);
