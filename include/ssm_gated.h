@@ -33,6 +33,9 @@
  *     narrower ones, others single elements, each slower than the one before.  bf16 pairs of channels also want A, h0, h_last,
  *     dh_last, dh0 and the saved states aligned to 8 bytes; otherwise single elements move.
  *   - Results are bitwise reproducible for the same problem, pointers' alignment and presence of optional arguments.
+ *   - The blocks that share a channel's sequence wait for one another, for a limited time.  A wait that runs out (a fault
+ *     elsewhere) leaves NaN in what its block writes from there on, h_last, dh0 and its share of dA included (not in steps that a
+ *     reset within the same tile cuts off).
  *   - NaN and Inf propagate along the recurrence (and not across a reset).  A > 0 is not validated and gives NaN.
  */
 #ifndef SSM_GATED_H_
@@ -46,8 +49,10 @@ extern "C" {
 
 enum {
   SSM_GATED_FLAG_DECAY = 1u,       /* the decay form: A and in_gate are given                                          */
-  SSM_GATED_FLAG_SAVE_STATES = 4u  /* forward: also write the states that backward restarts from; backward: they are
+  SSM_GATED_FLAG_SAVE_STATES = 4u, /* forward: also write the states that backward restarts from; backward: they are
                                       given (otherwise the call rebuilds them in its workspace)                       */
+  SSM_GATED_FLAG_TEST_WITHHOLD = 16u /* test hook for the bounded waits: where blocks exchange, one sends nothing, so that
+                                      the others' waits run out (at once)                                             */
 };
 
 typedef struct {
@@ -87,7 +92,7 @@ SSM_API ssm_status_t ssm_gated_bwd(const ssm_gated_problem_t* p, const void* x, 
 
 /*
  * One step of decoding: x, gate, in_gate and y hold one row per batch entry, h [batch][D] is updated in place.  p->L must be
- * 1; in_gate and A as in the forward call; reset [batch] may be NULL.  SSM_GATED_FLAG_SAVE_STATES is refused.
+ * 1; in_gate and A as in the forward call; reset [batch] may be NULL.  Flags other than SSM_GATED_FLAG_DECAY are refused.
  */
 SSM_API ssm_status_t ssm_gated_step(const ssm_gated_problem_t* p, const void* x, const void* gate, const void* in_gate,
                                     const float* A, const uint8_t* reset, float* h, void* y,

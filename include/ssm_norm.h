@@ -19,7 +19,8 @@
  * weight, bias, dweight, dbias float32 [D]; stats float32 [rows][2] (m, r).  Arithmetic and sums are float32.  Every
  * pointer is aligned to its element; rows of whole 16 bytes at aligned pointers (to 16 bytes, float32 ones beside bf16 io to 32)
  * take wide accesses, bf16 rows of whole pairs (4 and 8 bytes) narrower ones.
- * NaN and Inf propagate within their row (and into dweight and dbias).
+ * NaN and Inf propagate within their row (and into dweight and dbias).  The backward call waits for its own copies of long rows, for
+ * a limited time; a wait that runs out (a fault elsewhere) leaves NaN in the row, in those after it, in dweight and in dbias.
  */
 #ifndef SSM_NORM_H_
 #define SSM_NORM_H_
@@ -33,7 +34,9 @@ extern "C" {
 enum {
   SSM_NORM_FLAG_RMS = 1u,          /* no mean is subtracted                                     */
   SSM_NORM_FLAG_HAS_BIAS = 2u,     /* bias is given; otherwise 0 and dbias not produced         */
-  SSM_NORM_FLAG_HAS_RESIDUAL = 4u  /* residual is given                                         */
+  SSM_NORM_FLAG_HAS_RESIDUAL = 4u, /* residual is given                                         */
+  SSM_NORM_FLAG_TEST_WITHHOLD = 16u /* test hook for the bounded waits of backward: where rows come by copies that are waited
+                                      for, one stays away, so that the waits run out (at once) */
 };
 
 typedef struct {

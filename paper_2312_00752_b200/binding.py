@@ -38,8 +38,8 @@ SSM_STATIC_SCRATCH_BYTES = 4 << 20
 
 
 SSM_CONV_FLAG_SILU, SSM_CONV_FLAG_HAS_BIAS = 1, 2
-SSM_GATED_FLAG_DECAY, SSM_GATED_FLAG_SAVE_STATES = 1, 4
-SSM_NORM_FLAG_RMS, SSM_NORM_FLAG_HAS_BIAS, SSM_NORM_FLAG_HAS_RESIDUAL = 1, 2, 4
+SSM_GATED_FLAG_DECAY, SSM_GATED_FLAG_SAVE_STATES, SSM_GATED_FLAG_TEST_WITHHOLD = 1, 4, 16
+SSM_NORM_FLAG_RMS, SSM_NORM_FLAG_HAS_BIAS, SSM_NORM_FLAG_HAS_RESIDUAL, SSM_NORM_FLAG_TEST_WITHHOLD = 1, 2, 4, 16
 
 
 class ssm_conv_problem_t(ctypes.Structure):

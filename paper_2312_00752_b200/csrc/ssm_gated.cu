@@ -54,7 +54,7 @@ int64_t row_distance(int64_t ld, int D) { return ld == 0 ? D : ld; }
 
 ssm_status_t validate(const ssm_gated_problem_t* p) {
   if (p == nullptr || p->batch < 1 || p->L < 1 || p->D < 1) return SSM_ERR_INVALID_ARG;
-  if (p->flags & ~(uint32_t)(SSM_GATED_FLAG_DECAY | SSM_GATED_FLAG_SAVE_STATES)) return SSM_ERR_INVALID_ARG;
+  if (p->flags & ~(uint32_t)(SSM_GATED_FLAG_DECAY | SSM_GATED_FLAG_SAVE_STATES | SSM_GATED_FLAG_TEST_WITHHOLD)) return SSM_ERR_INVALID_ARG;
   if (p->io_dtype != SSM_F32 && p->io_dtype != SSM_BF16) return SSM_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)p->batch * p->L;
   if (p->D > 1 << 28 || rows > INT64_MAX >> 32) return SSM_ERR_UNSUPPORTED;   // (byte offsets stay within 63 bits)
@@ -77,6 +77,7 @@ GatedParams params(const ssm_gated_problem_t& p) {
   g.L = p.L;
   g.D = p.D;
   g.nck = (p.L + kGatedSteps - 1) / kGatedSteps;
+  g.withhold = p.flags & SSM_GATED_FLAG_TEST_WITHHOLD ? 1 : 0;
   g.ld_x = row_distance(p.ld_x, p.D);
   g.ld_gate = row_distance(p.ld_gate, p.D);
   g.ld_in = row_distance(p.ld_in_gate, p.D);
@@ -202,7 +203,7 @@ ssm_status_t ssm_gated_step(const ssm_gated_problem_t* p, const void* x, const v
   const ssm_status_t st = validate(p);
   if (st != SSM_OK) return st;
   const bool dec = decay(*p);
-  if (p->L != 1 || (p->flags & SSM_GATED_FLAG_SAVE_STATES) || !x || !gate || !h || !y || dec != (in_gate != nullptr) ||
+  if (p->L != 1 || (p->flags & ~(uint32_t)SSM_GATED_FLAG_DECAY) || !x || !gate || !h || !y || dec != (in_gate != nullptr) ||
       dec != (A != nullptr))
     return SSM_ERR_INVALID_ARG;
   const size_t esz = esize(*p);

@@ -33,6 +33,7 @@ struct GatedParams {
   int64_t ld_x, ld_gate, ld_in, ld_dx, ld_dgate, ld_din;   // distance of rows, in elements
   int batch, L, D, nck;
   int tiles;              // groups of channels of one batch entry
+  int withhold;           // test hook: the first block of a cluster has given up from the start, the others wait briefly
 };
 
 #ifdef __CUDACC__
@@ -201,10 +202,14 @@ __device__ __forceinline__ void barrier_expect(const void* barrier, unsigned byt
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
 }
 // Waits for the bytes of a phase.  The blocks of a cluster run at the same time and send before they wait, so that every wait
-// ends; the limit (seconds) keeps a fault elsewhere from holding the GPU.  False: it was reached.
-constexpr int kWaitLimit = 1 << 20;
-__device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase) {
-  for (int i = 0; i < kWaitLimit; ++i) {
+// ends; the limit (4 us a turn, 4 s) keeps a fault elsewhere from holding the GPU.  False: it was reached.  A thread that has given
+// up sets its limit to 0.  It waits no more than one turn, expects no further bytes (the phase is still open) and sends none, so that
+// the others give up as well, and the bytes that arrive uncounted are those of a round or two.  From there on its carry is NaN, which
+// stays by itself but where a reset lets nothing pass, and its block stays until the others have left or given up too.
+constexpr int kWaitLimit = 1 << 20, kWithheldLimit = 1000;
+__device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase, int limit) {
+  int i = 0;
+  do {
     unsigned done;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -212,7 +217,7 @@ __device__ __forceinline__ bool barrier_wait(const void* barrier, unsigned phase
         : "r"(shared_address(barrier)), "r"(phase)
         : "memory");
     if (done) return true;
-  }
+  } while (++i < limit);
   return false;
 }
 

@@ -64,7 +64,7 @@ struct Feed {
   __device__ __forceinline__ void rows(int n, int stage) {
 #pragma unroll
     for (int i = 0; i < kTensors; ++i) {
-#pragma unroll
+#pragma unroll(COPY == 4 && sizeof(IO) == 2 ? 4 : S / kRows)   // (pairs of bf16: all eight need more registers than there are)
       for (int k = 0; k < S / kRows; ++k) {
         const int row = k * kRows + lane / kLanes;
         const char* src = next[i] + (uint64_t)ld[i] * (k * kRows);
@@ -166,6 +166,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
   auto state_at = [&](int k) { return live && k >= 0 ? *reinterpret_cast<const F*>(ps + (int64_t)k * p.D) : vset<F>(0.f); };
   F h0 = state_at(q), h1 = state_at(q - step);       // saved states of this run and the next
   F A = vset<F>(0.f), carry = vset<F>(0.f), dA = vset<F>(0.f);   // carry: what enters the round from the future
+  int limit = !p.withhold ? kWaitLimit : rank > 0 ? kWithheldLimit : 0;   // of the waits; 0: one has been given up
   if (live) {
     if constexpr (DECAY) A = *reinterpret_cast<const F*>(p.A + d);
     if (p.dh_last != nullptr) carry = *reinterpret_cast<const F*>(p.dh_last + (int64_t)b * p.D + d);
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
     if (!RESET || cuts == 0) mine.P = vmap(mine.P, [](float v) { return fmaxf(v, FLT_MIN); });
 
     s_warp[half][w][lane] = mine;
-    if (C > 1 && threadIdx.x == 0) barrier_expect(&s_there[half], C * 32 * sizeof(Affine<F>));
+    if (C > 1 && threadIdx.x == 0 && limit > 0) barrier_expect(&s_there[half], C * 32 * sizeof(Affine<F>));
     __syncthreads();
     F c;
     if (C == 1) {
@@ -262,17 +263,21 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
 #pragma unroll
       for (int j = 1; j < W - 1; ++j)
         if (j < w) ahead = then<RESET>(ahead, s_warp[half][j][lane]);
-      if (w == W - 1) {
+      if (w == W - 1 && limit > 0) {
         const Affine<F> all = then<RESET>(ahead, mine);
         for (int j = 0; j < C; ++j) send(remote_address(&s_block[half][rank][lane], j), remote_address(&s_there[half], j), all);
       }
-      if (!barrier_wait(&s_there[half], r >> 1 & 1)) carry = vset<F>(NAN);
+      if (!barrier_wait(&s_there[half], r >> 1 & 1, limit)) {
+        limit = 0;
+        carry = vset<F>(NAN);
+      }
       F enter = carry;
       for (int j = 0; j < C; ++j) {
         if (j == rank) enter = carry;
         carry = apply<RESET>(s_block[half][j][lane], carry);
       }
       c = w == 0 ? enter : apply<RESET>(ahead, enter);
+      if (RESET && limit == 0) c = carry = vset<F>(NAN);
     }
 
     if (n > 0) {
@@ -326,6 +331,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
     in.release();
     if constexpr (COPY > 0) in.issue(rows_of(q - 2 * step), half, step * S);
   }
+  if (__any_sync(~0u, limit == 0)) cluster_sync();       // (waits for the blocks that have not left)
   if (p.dh0 != nullptr && live && w == 0 && rank == 0) *reinterpret_cast<F*>(p.dh0 + (int64_t)b * p.D + d) = carry;
   if constexpr (DECAY) {                             // the warps' sums of dA, in order
     __syncthreads();

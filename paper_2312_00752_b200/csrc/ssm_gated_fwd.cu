@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(32 * W, DECAY && !RESET ? 3 : 4) ssm_gated_fwd
   auto mask_at = [&](int t) -> unsigned { return RESET && lane < S && t + lane < p.L ? pr[t + lane] : 0u; };
   unsigned mask0 = mask_at(t0), mask1 = mask_at(t0 + step);
   F A = vset<F>(0.f), carry = vset<F>(0.f);          // carry: the state that enters the round
+  int limit = !p.withhold ? kWaitLimit : rank > 0 ? kWithheldLimit : 0;   // of the waits; 0: one has been given up
   if (live) {
     if constexpr (DECAY) A = *reinterpret_cast<const F*>(p.A + d);
     if (p.h0 != nullptr) carry = *reinterpret_cast<const F*>(p.h0 + (int64_t)b * p.D + d);
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(32 * W, DECAY && !RESET ? 3 : 4) ssm_gated_fwd
     if (!RESET || cuts == 0) mine.P = vmap(mine.P, [](float v) { return fmaxf(v, FLT_MIN); });
 
     s_warp[half][w][lane] = mine;
-    if (C > 1 && threadIdx.x == 0) barrier_expect(&s_there[half], C * 32 * sizeof(Affine<F>));
+    if (C > 1 && threadIdx.x == 0 && limit > 0) barrier_expect(&s_there[half], C * 32 * sizeof(Affine<F>));
     __syncthreads();
     F h;
     if (C == 1) {
@@ -212,17 +213,21 @@ __global__ void __launch_bounds__(32 * W, DECAY && !RESET ? 3 : 4) ssm_gated_fwd
 #pragma unroll
       for (int j = 1; j < W - 1; ++j)
         if (j < w) before = then<RESET>(before, s_warp[half][j][lane]);
-      if (w == W - 1) {
+      if (w == W - 1 && limit > 0) {
         const Affine<F> all = then<RESET>(before, mine);
         for (int j = 0; j < C; ++j) send(remote_address(&s_block[half][rank][lane], j), remote_address(&s_there[half], j), all);
       }
-      if (!barrier_wait(&s_there[half], r >> 1 & 1)) carry = vset<F>(NAN);
+      if (!barrier_wait(&s_there[half], r >> 1 & 1, limit)) {
+        limit = 0;
+        carry = vset<F>(NAN);
+      }
       F enter = carry;
       for (int j = 0; j < C; ++j) {
         if (j == rank) enter = carry;
         carry = apply<RESET>(s_block[half][j][lane], carry);
       }
       h = w == 0 ? enter : apply<RESET>(before, enter);
+      if (RESET && limit == 0) h = carry = vset<F>(NAN);
     }
 
     if (live && n > 0) {
@@ -245,6 +250,7 @@ __global__ void __launch_bounds__(32 * W, DECAY && !RESET ? 3 : 4) ssm_gated_fwd
       }
     }
   }
+  if (__any_sync(~0u, limit == 0)) cluster_sync();       // (waits for the blocks that have not left)
   if (p.h_last != nullptr && live && w == 0 && rank == 0) *reinterpret_cast<F*>(p.h_last + (int64_t)b * p.D + d) = carry;
 }
 

@@ -32,6 +32,7 @@ struct NormParams {
   int D, rms;
   float eps;
   int rows_per_part;         // (the kernels for long rows)
+  int withhold;              // test hook: the ring's first row stays incomplete, and is waited for briefly
   int group;                 // threads of a row: a power of two up to 32, or a multiple of 32 that is the whole block
 };
 
@@ -417,11 +418,12 @@ __device__ __forceinline__ void bulk_load(const void* dst, const void* src, unsi
 __device__ __forceinline__ void expect(const uint64_t* barrier, unsigned bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
 }
-// Waits for a row.  Its copies are under way when the wait begins, so that it ends; the limit (seconds) is for a fault elsewhere,
-// and what would be made of the row is NaN then.
-constexpr int kWaitLimit = 1 << 20;
-__device__ __forceinline__ bool wait_full(const uint64_t* barrier, unsigned phase) {
-  for (int i = 0; i < kWaitLimit; ++i) {
+// Waits for a row.  Its copies are under way when the wait begins, so that it ends; the limit (4 s) is for a fault elsewhere.  A thread that
+// has given up waits and fetches no more, and makes NaN of its columns: of dx from this row on (of the whole row, by the sums), of
+// its share of dweight and dbias.
+constexpr int kWaitLimit = 1 << 20, kWithheldLimit = 1000;
+__device__ __forceinline__ bool wait_full(const uint64_t* barrier, unsigned phase, int limit) {
+  for (int i = 0; i < limit; ++i) {
     unsigned done;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(done)
@@ -446,12 +448,13 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
   if (threadIdx.x == 0) set_up_barriers(s_full, stages);
   __syncthreads();
   dependency_wait();
+  const int limit = p.withhold ? kWithheldLimit : kWaitLimit;
   auto fill = [&](int64_t row, int stage) {                // thread 0
     if (row >= p.rows) return;
     char* dst = s_ring + stage * bytes;
     expect(&s_full[stage], bytes);
     bulk_load(dst, static_cast<const RES*>(p.s) + row * p.D, sbytes, &s_full[stage]);
-    bulk_load(dst + sbytes, static_cast<const IO*>(p.dy) + row * p.D, ybytes, &s_full[stage]);
+    if (!(p.withhold && row < gridDim.x)) bulk_load(dst + sbytes, static_cast<const IO*>(p.dy) + row * p.D, ybytes, &s_full[stage]);
     if (add) bulk_load(dst + sbytes + ybytes, static_cast<const RES*>(p.dresidual_out) + row * p.D, sbytes, &s_full[stage]);
   };
   if (threadIdx.x == 0)
@@ -467,9 +470,11 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
   int stage = 0, turn = 0;
   unsigned phase = 0;
   const float over = 1.f / (float)p.D;
+  bool there = true;                                       // no wait has been given up
   float mn = p.stats[2 * (int64_t)blockIdx.x], rn = p.stats[2 * (int64_t)blockIdx.x + 1];
   for (int64_t here = blockIdx.x; here < p.rows; here += gridDim.x, turn ^= 1) {
-    const float m = mn, r = rn;
+    const float m = mn;
+    float r = rn;
     if (here + gridDim.x < p.rows) {
       mn = p.stats[2 * (here + gridDim.x)];
       rn = p.stats[2 * (here + gridDim.x) + 1];
@@ -478,9 +483,21 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
     const RES* bs = reinterpret_cast<const RES*>(at);
     const IO* by = reinterpret_cast<const IO*>(at + sbytes);
     const RES* ba = reinterpret_cast<const RES*>(at + sbytes + ybytes);
-    const bool there = wait_full(&s_full[stage], phase);
+    if (there && !wait_full(&s_full[stage], phase, limit)) {
+      there = false;
+      if (threadIdx.x == 0)                                // the copies under way are waited for, if they come at all
+        for (int i = 0; i < stages - 1; ++i)
+          if (here + (int64_t)i * gridDim.x < p.rows)
+            wait_full(&s_full[stage + i < stages ? stage + i : stage + i - stages], stage + i < stages ? phase : phase ^ 1, limit);
+      if constexpr (BIAS)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int i = 0; i < M; ++i) db[k][i] = vset<F>(NAN);
+    }
+    if (!there) r = NAN;
     const F off = vset<F>(-m);
-    F acc0 = vset<F>(there ? 0.f : NAN), acc1 = acc0;
+    F acc0 = vset<F>(0.f), acc1 = acc0;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * group + j) * VE;
@@ -508,8 +525,8 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
     float sum[2] = {total(acc0), total(acc1)};
     group_sum(sum, group, s_sum, turn);
     // every thread is past the row before this one: its place is free
-    if (threadIdx.x == 0) fill(here + (int64_t)(stages - 1) * gridDim.x, stage == 0 ? stages - 1 : stage - 1);
-    const float c1 = p.rms ? (there ? 0.f : NAN) : sum[0] * over, c2 = sum[1] * over;
+    if (threadIdx.x == 0 && there) fill(here + (int64_t)(stages - 1) * gridDim.x, stage == 0 ? stages - 1 : stage - 1);
+    const float c1 = p.rms ? 0.f : sum[0] * over, c2 = sum[1] * over;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * group + j) * VE;
@@ -673,7 +690,7 @@ constexpr int kMaxParts = 148 * 4;
 
 ssm_status_t validate(const ssm_norm_problem_t* p) {
   if (p == nullptr || p->rows < 1 || p->D < 1) return SSM_ERR_INVALID_ARG;
-  if (p->flags & ~(uint32_t)(SSM_NORM_FLAG_RMS | SSM_NORM_FLAG_HAS_BIAS | SSM_NORM_FLAG_HAS_RESIDUAL)) return SSM_ERR_INVALID_ARG;
+  if (p->flags & ~(uint32_t)(SSM_NORM_FLAG_RMS | SSM_NORM_FLAG_HAS_BIAS | SSM_NORM_FLAG_HAS_RESIDUAL | SSM_NORM_FLAG_TEST_WITHHOLD)) return SSM_ERR_INVALID_ARG;
   if (!(p->eps >= 0.f && p->eps <= 3.0e38f)) return SSM_ERR_INVALID_ARG;
   if (p->io_dtype != SSM_F32 && p->io_dtype != SSM_BF16) return SSM_ERR_UNSUPPORTED;
   if (p->residual_dtype != SSM_F32 && p->residual_dtype != SSM_BF16) return SSM_ERR_UNSUPPORTED;
@@ -938,6 +955,7 @@ ssm_status_t ssm_norm_bwd(const ssm_norm_problem_t* p, const void* sum, const fl
   n.rows = p->rows;
   n.D = p->D;
   n.rms = p->flags & SSM_NORM_FLAG_RMS ? 1 : 0;
+  n.withhold = p->flags & SSM_NORM_FLAG_TEST_WITHHOLD ? 1 : 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int parts = 0;
   cudaError_t e;
