@@ -470,11 +470,10 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
   int stage = 0, turn = 0;
   unsigned phase = 0;
   const float over = 1.f / (float)p.D;
-  bool there = true;                                       // no wait has been given up
+  int gave_up = 0;                                         // 1 + 2 stage + phase of the wait that ran out
   float mn = p.stats[2 * (int64_t)blockIdx.x], rn = p.stats[2 * (int64_t)blockIdx.x + 1];
   for (int64_t here = blockIdx.x; here < p.rows; here += gridDim.x, turn ^= 1) {
-    const float m = mn;
-    float r = rn;
+    const float m = mn, r = rn;
     if (here + gridDim.x < p.rows) {
       mn = p.stats[2 * (here + gridDim.x)];
       rn = p.stats[2 * (here + gridDim.x) + 1];
@@ -483,21 +482,10 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
     const RES* bs = reinterpret_cast<const RES*>(at);
     const IO* by = reinterpret_cast<const IO*>(at + sbytes);
     const RES* ba = reinterpret_cast<const RES*>(at + sbytes + ybytes);
-    if (there && !wait_full(&s_full[stage], phase, limit)) {
-      there = false;
-      if (threadIdx.x == 0)                                // the copies under way are waited for, if they come at all
-        for (int i = 0; i < stages - 1; ++i)
-          if (here + (int64_t)i * gridDim.x < p.rows)
-            wait_full(&s_full[stage + i < stages ? stage + i : stage + i - stages], stage + i < stages ? phase : phase ^ 1, limit);
-      if constexpr (BIAS)
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-          for (int i = 0; i < M; ++i) db[k][i] = vset<F>(NAN);
-    }
-    if (!there) r = NAN;
+    if (gave_up == 0 && !wait_full(&s_full[stage], phase, limit)) gave_up = 1 + 2 * stage + (int)phase;
+    const bool there = gave_up == 0;
     const F off = vset<F>(-m);
-    F acc0 = vset<F>(0.f), acc1 = acc0;
+    F acc0 = vset<F>(there ? 0.f : NAN), acc1 = acc0;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * group + j) * VE;
@@ -526,7 +514,7 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
     group_sum(sum, group, s_sum, turn);
     // every thread is past the row before this one: its place is free
     if (threadIdx.x == 0 && there) fill(here + (int64_t)(stages - 1) * gridDim.x, stage == 0 ? stages - 1 : stage - 1);
-    const float c1 = p.rms ? 0.f : sum[0] * over, c2 = sum[1] * over;
+    const float c1 = p.rms ? (there ? 0.f : NAN) : sum[0] * over, c2 = sum[1] * over;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * group + j) * VE;
@@ -565,6 +553,20 @@ __global__ void __launch_bounds__(bwd_threads(VE, NV)) ssm_norm_ring_bwd_kernel(
       stage = 0;
       phase ^= 1;
     }
+  }
+  if (gave_up > 0) {
+    // (thread 0: the copies under way were of this stage's row and of the stages - 2 after it)
+    for (int i = 0; threadIdx.x == 0 && i < stages - 1; ++i) {
+      const int at = (gave_up - 1) / 2 + i, back = at < stages ? at : at - stages;
+      wait_full(&s_full[back], (unsigned)(((gave_up - 1) & 1) ^ (at < stages ? 0 : 1)), limit);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        dw[k][i] = vset<F>(NAN);
+        if constexpr (BIAS) db[k][i] = vset<F>(NAN);
+      }
   }
   block_parts<VE, NV>(p.dw_part + (size_t)blockIdx.x * p.D, dw, p.D, group, nullptr);
   if constexpr (BIAS) block_parts<VE, NV>(p.db_part + (size_t)blockIdx.x * p.D, db, p.D, group, nullptr);
