@@ -109,10 +109,13 @@ struct Feed {
 
 // 1 - g of a gate g = sigma(z).  Where g is near 1 the difference cancels: its absolute error is up to 2.5 * 2^-25 (the sum 1 + e, the
 // reciprocal and the difference are rounded), which is 3e-5 of it at z = kOpen, a hundredth of a bf16's rounding, and all of it at 17.
-// e g has no such limit and takes another exponential (exact).  float32 io always forms it so; with bf16 it is 12 % of the kernel's
-// time ((8, 2048, 2560) 174 us, 154 without), so that a warp looks for gates above kOpen among its own first: 156.
+// e g has no such limit and takes another exponential (exact).  float32 io always forms it so where g is not small (it has twice the
+// bytes to wait for).  With bf16 a warp looks for gates above kOpen among its own first: (8, 2048, 2560) 155 us where it finds none,
+// 180 where every one is (154 and 181 if it never or always formed them so).
+// CLAMP: e is held finite instead of the difference taken where g is small (g is 0 where that matters, and the gradients are products
+// with it); 180 us against 187, but not for rows of pairs of bf16, (2, 2048, 1026) 33.5 against 31.6.
 constexpr float kOpen = 6.f;
-template <class F, class Exact>
+template <bool CLAMP, class F, class Exact>
 __device__ __forceinline__ F rest(F z, F g, Exact exact) {   // exact: bool, or known when compiled
   const F near = vfma(g, vset<F>(-1.f), vset<F>(1.f));
   if constexpr (std::is_same<Exact, bool>::value) {
@@ -120,7 +123,9 @@ __device__ __forceinline__ F rest(F z, F g, Exact exact) {   // exact: bool, or 
   } else if constexpr (!Exact::value) {
     return near;
   }
-  const F far = vmul(vmap(vmul(z, vset<F>(-kLog2e)), [](float v) { return ex2_approx(v); }), g);
+  const F v = vmul(z, vset<F>(-kLog2e));
+  if constexpr (CLAMP) return vmul(vmap(v, [](float v) { return ex2_approx(fminf(v, 126.f)); }), g);
+  const F far = vmul(vmap(v, [](float v) { return ex2_approx(v); }), g);
   return vmap(g, near, far, [](float v, float n, float f) { return v < 0.5f ? n : f; });
 }
 
@@ -134,6 +139,7 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
   constexpr int V = kWidth<F>;
   constexpr int kAhead = COPY > 0 ? 2 : 1;           // tiles fetched before the first is looked at
   constexpr bool kLook = DECAY && sizeof(IO) == 2;   // whether a gate is above kOpen is asked
+  constexpr bool kClamp = kLook && COPY == 16;
   extern __shared__ __align__(16) char s_feed[];
   __shared__ Affine<F> s_warp[2][W][32];
   __shared__ Affine<F> s_block[2][kGatedCluster][32];
@@ -299,10 +305,10 @@ __global__ void __launch_bounds__(32 * W, DECAY ? 3 : 4) ssm_gated_bwd_kernel(co
             } else {
               const F iota = vmul(wi[k], inv[k]);
               dx = vmul(mu, wi[k]);
-              di = vmul(vmul(dx, x), rest(in.get(DECAY ? 3 : 0, k, stage), iota, exact));
+              di = vmul(vmul(dx, x), rest<kClamp>(in.get(DECAY ? 3 : 0, k, stage), iota, exact));
               const F m = vmul(vmul(back, vfma(vmul(a[k], vset<F>(-1.f)), vmul(vmul(iota, inv[k]), x), before[k])), g[k]);   // m rho
               dA = vadd(dA, m);
-              dg = vmul(vmul(m, A), rest(in.get(1, k, stage), g[k], exact));
+              dg = vmul(vmul(m, A), rest<kClamp>(in.get(1, k, stage), g[k], exact));
             }
             if (live) {
               *reinterpret_cast<Raw*>(ox + (uint64_t)lx * k) = Io::close(dx);

@@ -54,3 +54,33 @@ def test_gradients_of_nearly_saturated_gates(batch, L, D, sign, A, io):
                 "dgate": -mu * a * a / beta * iota * x * decay * rho * closed}
     for name, ref in want.items():
         _near(y if name == "y" else g[name], ref, np.abs(ref), io)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("A", [-0.4, -3.0])
+@pytest.mark.parametrize("L,D", [(40, 100), (37, 101)])
+def test_gates_of_every_size(L, D, A, io):
+    # closed gates may flush to 0 what float32 cannot hold as a normal number, and the forward pass drops inputs whose gate is below -44
+    from paper_2312_00752_b200 import binding as K
+    levels = np.array([-200.0, -95.0, -87.0, -60.0, -30.0, -12.0, -5.0, 0.0, 6.0, 6.25, 12.0, 30.0, 60.0, 87.0, 95.0, 200.0])
+    rng = np.random.default_rng(D)
+    pick = lambda: rng.choice(levels, (1, L, D)).astype(np.float32)
+    n = lambda *s: synth.round_to_io(rng.standard_normal(s), io)
+    case = {"x": n(1, L, D), "gate": pick(), "in_gate": pick(), "A": (A * (1 - 0.5 * rng.random(D))).astype(np.float32),
+            "reset": np.ones((1, L), bool), "dy": n(1, L, D)}
+    d = device(case, io)
+    y, saved = K.ssm_gated_fwd(d["x"], d["gate"], d["in_gate"], d["A"], reset=d["reset"], save_states=True)
+    g = K.ssm_gated_bwd(d["x"], d["gate"], d["in_gate"], d["A"], d["dy"], saved, reset=d["reset"])
+    x, mu, decay = (case[k].astype(np.float64) for k in ("x", "dy", "A"))
+    (rho, closed), (iota, off) = (_sigma(case[k].astype(np.float64)) for k in ("gate", "in_gate"))
+    la = rho * decay
+    a, beta = np.exp(la), np.sqrt(-np.expm1(2 * la))
+    lost = 1e-18 * np.abs(x)        # (beta is at least 1e-19, the root of the least normal number; the gate's limit is 1e-19)
+    held = np.where(np.abs(la) > 1e-30, np.abs(la), 0.0)          # (below, the step size itself is no normal number any more)
+    slope = np.divide(a * a * iota * x * decay * rho * closed, beta, out=np.zeros_like(x), where=held > 0)
+    want = {"y": (beta * iota * x, lost), "dx": (mu * beta * iota, 1e-18 * np.abs(mu)),
+            "din_gate": (mu * beta * x * iota * off, 1e-18 * np.abs(mu * x)), "dgate": (-mu * slope, 1e-14 * np.abs(mu * x))}
+    for name, (ref, floor) in want.items():
+        got = (y if name == "y" else g[name]).detach().double().cpu().numpy()
+        over = np.abs(got - ref) - HALF[io] * np.abs(ref) - E * (1 + HALF[io]) * np.abs(ref) - floor
+        assert np.isfinite(got).all() and over.max() <= 0, (name, over.max(), np.unravel_index(over.argmax(), over.shape))
