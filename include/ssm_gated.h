@@ -28,7 +28,9 @@
  *     written.  y, dy: dense [batch][L][D] io_dtype.
  *   - A, dA float32 [D]; h0, h_last, dh_last, dh0 and the h of ssm_gated_step float32 [batch][D]; reset one byte per step,
  *     [batch][L] (ssm_gated_step: [batch]).
- *   - Arithmetic, states and sums are float32; y and the gradients of the inputs are rounded once to io_dtype.
+ *   - Arithmetic, states and sums are float32; y and the gradients of the inputs are rounded once to io_dtype.  (Decay
+ *     form: an in_gate below -44, which lets less than 1e-19 of its input through, may let nothing through in the forward pass and
+ *     the step.  The gradients of gates are good relative to their own size however far the gates are open.)
  *   - Every pointer is aligned to its element.  Rows that begin and end on 16 bytes take the widest copies, such on 4 bytes
  *     narrower ones, others single elements, each slower than the one before.  bf16 pairs of channels also want A, h0, h_last,
  *     dh_last, dh0 and the saved states aligned to 8 bytes; otherwise single elements move.
@@ -56,7 +58,7 @@ enum {
 };
 
 typedef struct {
-  int32_t batch, L, D;   /* all >= 1 */
+  int32_t batch, L, D;   /* all >= 1; D at most 2^28, batch * L below 2^31, batch * ceil(D / 32) below 2^27, L below 2^31 - 2^16 */
   int32_t io_dtype;      /* ssm_dtype_t */
   uint32_t flags;        /* SSM_GATED_FLAG_* */
   int64_t ld_x, ld_gate, ld_in_gate;      /* distance of rows in elements; 0: D.  Other than 0 only where it is used   */

@@ -101,8 +101,8 @@ __device__ __forceinline__ void decay_pair(F v, F& a, F& oa) {
   a = vmap(v, vfma(near, vset<F>(-1.f), vset<F>(1.f)), ex, [](float w, float n, float f) { return fabsf(w) < 0.25f ? n : f; });
 }
 
-// The same for -1 <= A <= 0, with w = -v in [0, 1]: (1 - exp(-w)) / w by its Chebyshev interpolation of degree 6 (relative error
-// 3e-9), no special-function operation and no case distinction.
+// The same for -1 <= A <= 0, with w = -v in [0, 1]: (1 - exp(-w)) / w by its Chebyshev interpolation of degree 6, the constant
+// term set to 1 (relative error 2.4e-8 at w = 1, less elsewhere: below half a unit), no special-function operation and no case distinction.
 template <class F>
 __device__ __forceinline__ void decay_pair_small(F w, F& a, F& oa) {
   F s = vfma(w, vset<F>(1.29076311e-4f), vset<F>(-1.30077498e-3f));
@@ -124,7 +124,8 @@ __device__ __forceinline__ F one_minus_square(F oa) {
 
 // One step of the forward recurrence: retention a and input u.  SMALL: -1 <= A <= 0, and A comes negated.
 // The special-function unit, four lanes a cycle, limits bf16 io next to the memory, so beta and the input gate come from
-// one operation: with f = 1 + exp(-in_gate), m2 rsqrt(m2 f^2) = sqrt(m2) / f = beta iota (f^2 may be infinite: then it is 0).
+// one operation: with f = 1 + exp(-in_gate), m2 rsqrt(m2 f^2) = sqrt(m2) / f = beta iota (f^2 is infinite below an
+// in_gate of -44 or less: then it is 0 instead of 1e-19 or less; the backward pass has iota by itself).
 template <bool DECAY, bool SMALL, class F>
 __device__ __forceinline__ void step_inputs(F x, F gate, F in_gate, F A, F& a, F& u) {
   F g;

@@ -12,8 +12,8 @@
 // take no special-function operation beyond the five of the gates.
 //
 // What bounds it: 10 or 14 bytes an element and the saved states, about 120 instructions for a pair of channels in the decay form,
-// and the registers of what waits for the adjoint: ten values a step and pair, 164 in all, three blocks an SM ((8, 2048, 2560) bf16
-// 154 us, 58 % of the copy bandwidth; four blocks of 128 registers 226, two 200).  The convex form keeps six and runs four
+// and the registers of what waits for the adjoint: ten values a step and pair, 168 in all, three blocks an SM ((8, 2048, 2560) bf16
+// 155 us, 57 % of the copy bandwidth; four blocks of 128 registers 226, two 200; with A < -1 164).  The convex form keeps six and runs four
 // blocks ((4, 2048, 5120) bf16 97 us, 66 %).
 #include <cmath>
 #include <type_traits>

@@ -10,7 +10,8 @@
 //
 // What bounds it: 6 (convex) or 8 (decay) bytes an element, 2 or 4 special-function operations and about 43 or 59 instructions for a
 // pair of channels.  (4, 2048, 5120) bf16: convex 52 us, 74 % of the copy bandwidth, lost in the balance of its blocks ((4, 2048,
-// 9472), whose groups of channels fill the GPU exactly, 91 %); decay 76 us, 68 %, FP32 pipe and issue.
+// 9472), whose groups of channels fill the GPU exactly, 91 %); decay 77 us, 67 %, fixed latencies at 9.6 warps an SM (162 registers; no pipe is above 50 %).
+// A channel with A < -1 sends its warp through the general form of the gates: (8, 2048, 2560) 90 us instead of 77.
 //
 // P may underflow although no retention is zero, and zero times an infinite state would be NaN where the steps one by one
 // keep it infinite: it is held at the least normal number, 2^-126 of the state at most, far below its rounding.  A step that
@@ -278,7 +279,8 @@ cudaError_t launch_form(const GatedParams& p, bool decay, cudaStream_t s) {
 // A block takes a round's time and a half to get going, and the last blocks run faster when they are few, so that blocks in
 // 2.2 turns cost less than in three: 0.3 of the whole turns and 0.7 of the exact ones fit what clusters of 1 to 8 blocks measured
 // on 21 shapes of both kernels (the choice is 1 % off the best on the average, 6 % at most; clusters of two powers alone were 4 %
-// and 20 %).  Clusters lie within a GPC and leave places unused: per cent of the SMs' places that they can take.
+// and 20 %).  Clusters lie within a GPC and leave places unused: per cent of the SMs' places that they can take, measured with four blocks
+// an SM; for the kernels with three it is an estimate ((1, 131072, 1536) runs in clusters of 12).
 int choose_gated_cluster(long long groups, long long steps, int tile_steps, long long resident) {
   constexpr struct {
     int blocks, share;
